@@ -476,6 +476,183 @@ typedef struct hook_reduce_args {
 hook_status hook_reduce_mass(const hook_reduce_args* args);
 
 /*
+ * Rotary positions of queries and keys, with up to four axes (text: one; images and video: time, height and
+ * width), as the projections leave them and as hook_attn_probe and the paged cache expect them.  Pair c of a head turns by the
+ * angle
+ *   a(t, c) = positions[axis(c), t] * inv_freq[c]          c in [0, rotary_dim / 2)
+ *   (x1, x2) -> m * (x1 cos a - x2 sin a, x2 cos a + x1 sin a)       m = magnitude, or 1 where that is 0
+ * and with `inverse` by -a (captured queries and keys turned back; also the gradient of the rotation with respect to its
+ * input, for m = 1).  Elements rotary_dim .. head_dim - 1 of a head pass unchanged.  The angle is reduced in fp64, so far positions lose
+ * nothing; the rotation is computed in fp32 and rounded once, to nearest even.
+ *   layout      HOOK_ROPE_HALVES: pair c is elements c and c + rotary_dim / 2; HOOK_ROPE_NEIGHBOURS: 2c and 2c + 1
+ *   axis_order  HOOK_ROPE_BLOCKED: the first axis_pairs[0] pairs belong to axis 0, the next axis_pairs[1] to axis 1, ...;
+ *               HOOK_ROPE_CYCLIC: pair c belongs to axis c mod num_axes while that axis has pairs left (c / num_axes <
+ *               axis_pairs[that axis]), else to axis 0.  axis_pairs sum to rotary_dim / 2 in both; in the second every axis
+ *               but the first has to find all of its pairs below rotary_dim / 2.
+ * Rows are num_tokens rows of [heads, head_dim], one row's heads back to back, rows `*_stride` elements apart (0: back to back as
+ * well), so q, k and v may lie side by side in one buffer.  q and k may each be null (not rotated).  An output may be its own
+ * input (the same pointer and stride); otherwise outputs share no element with inputs or each other.
+ *
+ * With k_cache and v_cache given, the call also does what hook_kv_write would do with the rotated keys and with v:
+ * the rows go to the slots of the batch's new tokens (num_tokens = cu_q_lens[num_seqs]), bit for bit as by the two calls,
+ * quantised for an 8-bit cache; tokens are dropped by the same rules.  k_out may then be null (the keys go to the cache alone).
+ * Any head_dim up to HOOK_ROPE_MAX_DIM and any even rotary_dim; rows, halves and pointers that are multiples of 16 bytes run at
+ * full speed, others at that of the largest power of two that divides them.  Pointers are aligned to their elements.
+ */
+#define HOOK_ROPE_MAX_AXES 4
+#define HOOK_ROPE_MAX_DIM 512
+typedef enum hook_rope_layout { HOOK_ROPE_HALVES = 0, HOOK_ROPE_NEIGHBOURS = 1 } hook_rope_layout;
+typedef enum hook_rope_order { HOOK_ROPE_BLOCKED = 0, HOOK_ROPE_CYCLIC = 1 } hook_rope_order;
+
+typedef struct hook_rope_args {
+  int32_t num_tokens, num_q_heads, num_kv_heads, head_dim, rotary_dim;
+  int32_t num_axes;                         /* 1..HOOK_ROPE_MAX_AXES */
+  int32_t axis_pairs[HOOK_ROPE_MAX_AXES];
+  int32_t layout, axis_order;               /* hook_rope_layout, hook_rope_order */
+  int32_t inverse;
+  int32_t dtype;                            /* hook_dtype of q, k, v and the outputs */
+  float   magnitude;
+  const int32_t* positions;                 /* [num_axes, num_tokens] */
+  const float*   inv_freq;                  /* [rotary_dim / 2] */
+  const void*    q;                         /* [num_tokens, Hq, d], rows q_stride elements apart */
+  const void*    k;                         /* [num_tokens, Hkv, d] */
+  void*          q_out;
+  void*          k_out;
+  int64_t        q_stride, k_stride, q_out_stride, k_out_stride;
+  /* the cache write (all zero / null: none) */
+  int32_t        num_seqs, block_size, max_blocks_per_seq, num_blocks;
+  const void*    v;                         /* [num_tokens, Hkv, d] */
+  int64_t        v_stride;
+  const int32_t* block_table;               /* as for hook_kv_write */
+  const int32_t* seq_lens;
+  const int32_t* cu_q_lens;
+  void*          k_cache;
+  void*          v_cache;
+  int32_t        kv_dtype;                  /* hook_kv_dtype */
+  const float*   k_scale;                   /* [Hkv] */
+  const float*   v_scale;
+  void*          stream;
+} hook_rope_args;
+
+hook_status hook_rope(const hook_rope_args* args);
+
+/*
+ * Pages of a paged cache shared by several sequences.  A page is one block of every cache (each layer's keys and values); row i
+ * of a block table holds its first ceil(seq_lens[i] / 16) entries, and ref_counts[p] says how many rows (and other holders that
+ * the program counts itself, a kept prefix for example) hold page p; 0 is free.  The three calls keep tables, lengths and counts
+ * consistent on the device without the host seeing any of them:
+ *
+ *   hook_pages_fork     row j of the new table takes the first min(src_lens[j], L) tokens (all L where src_lens is null) of row
+ *                       src_rows[j] of the old one, or becomes empty where that is -1.  The new table replaces the old one:
+ *                       ref_counts[p] changes by the rows that hold p afterwards less those that did before.  So
+ *                       one call starts samples (a row named several times), reorders beams, shares or cuts back to a
+ *                       prefix, and frees (rows named by nobody).  No cache is touched: pages are shared until written.
+ *   hook_pages_append   room for n_i = cu_q_lens[i + 1] - cu_q_lens[i] new tokens: seq_lens grow by n_i and the rows get the pages
+ *                       they lack.  A last page that has to take new tokens but is held by others too is copied first: in the
+ *                       order of the rows, a row copies it while ref_counts says that more rows hold it than the row itself,
+ *                       and each copy takes one from that count (so the last holder keeps the page).  Its first L_i mod 16
+ *                       token rows are copied in every cache; the other rows of the new page stay as they are.  New pages are
+ *                       the lowest free ones, in the order of the rows, a row's copy before its further pages.  The call
+ *                       is all or nothing: with too few free pages, or a row longer than the table, nothing changes
+ *                       (outputs that are not the inputs receive the old values) and HOOK_PAGES_FULL is reported.
+ *   hook_pages_compact  the live pages are moved to pages 0 .. live - 1: the k-th lowest live page at or above `live` goes to the k-th
+ *                       lowest free page below it, in every cache; tables and counts follow.  page_map[p] is the new number of
+ *                       page p (-1: free) for holders outside the table; num_live receives `live`.
+ *
+ * Entries of a table behind a row's pages are neither read nor written.  *status collects what the calls find (bits are added,
+ * never cleared: zero the word once and look at it when convenient); the calls make what they find safe:
+ */
+typedef enum hook_pages_status {
+  HOOK_PAGES_FULL = 1,       /* append: too few free pages, or a row longer than the table; nothing was done */
+  HOOK_PAGES_BAD_ROW = 2,    /* fork: src_rows[j] outside [-1, num_seqs); the new row is empty */
+  HOOK_PAGES_BAD_LENGTH = 4, /* a length outside [0, max_blocks_per_seq * 16], taken as the nearest of these, or a negative n_i, taken as 0 */
+  HOOK_PAGES_BAD_PAGE = 8    /* a page that a row holds is outside [0, num_blocks) (its number is carried along), or, in
+                                hook_pages_compact, free (the entry is carried along) */
+} hook_pages_status;
+
+#define HOOK_PAGES_MAX_CACHES 256
+
+/*
+ * block_table_out and seq_lens_out of a fork are other buffers than the inputs (rows change places); those of the other two calls and
+ * ref_counts_out may be the inputs (the usual way to run them) or share nothing with them.  Arrays a call does not name are ignored.
+ * All arrays are DEVICE pointers but `caches`, a HOST array of num_caches device pointers, read before the call returns; each cache is
+ * [num_blocks, num_kv_heads, 16, row_bytes] bytes, 16-byte aligned, row_bytes (head_dim times the element's size) a multiple of 16.
+ * num_caches = 0 leaves the data alone; more than HOOK_PAGES_MAX_CACHES are refused.
+ */
+typedef struct hook_pages_args {
+  int32_t num_seqs, max_blocks_per_seq, num_blocks, block_size;
+  const int32_t* block_table;      /* [num_seqs, max_blocks_per_seq] */
+  const int32_t* seq_lens;         /* [num_seqs] */
+  const int32_t* ref_counts;       /* [num_blocks] */
+  int32_t*       block_table_out;  /* fork: [num_rows, max_blocks_per_seq], else as block_table */
+  int32_t*       seq_lens_out;     /* fork: [num_rows], append: [num_seqs] */
+  int32_t*       ref_counts_out;   /* [num_blocks] */
+  int32_t*       status;           /* [1] */
+  /* fork */
+  int32_t        num_rows;
+  const int32_t* src_rows;         /* [num_rows] */
+  const int32_t* src_lens;         /* [num_rows] or null */
+  /* append */
+  const int32_t* cu_q_lens;        /* [num_seqs + 1] */
+  /* compact */
+  int32_t*       page_map;         /* [num_blocks] */
+  int32_t*       num_live;         /* [1] */
+  /* append, compact: the data, and scratch memory (16-byte aligned; nothing in it needs to be set or kept) */
+  int32_t        num_caches, num_kv_heads;
+  int64_t        row_bytes;
+  void* const*   caches;           /* HOST array [num_caches] of device pointers */
+  void*          workspace;
+  size_t         workspace_bytes;  /* hook_pages_workspace_bytes(args) or more */
+  void*          stream;
+} hook_pages_args;
+
+/* Scratch bytes of hook_pages_append and hook_pages_compact for num_seqs rows and num_blocks pages (reads only these). */
+size_t hook_pages_workspace_bytes(const hook_pages_args* args);
+hook_status hook_pages_fork(const hook_pages_args* args);
+hook_status hook_pages_append(const hook_pages_args* args);
+hook_status hook_pages_compact(const hook_pages_args* args);
+
+/*
+ * Active programming of what the model answers with: penalties for repeated tokens, a bias list and a grammar mask on the logits.
+ * For row i and token t, with seen = t occurs in row i's history, and c = its occurrences there from entry prompt_lens[i] on (what has been
+ * generated; the entries before are the prompt):
+ *   x = logits[i, t]
+ *   seen:      x = x > 0 ? x / repetition[i] : x * repetition[i]
+ *   c > 0:     x = x - c * frequency[i] - presence[i]
+ *   biased:    x = x + the value of the last entry of row i's bias list that names t
+ *   barred:    x = -infinity                      (row i has a mask and bit t of it is 0; whatever x was)
+ *   out[i, t] = x, computed in fp32 and rounded once
+ * A token that none of these touches is copied bit for bit.  A mask that allows nothing leaves a row of -infinity.  Tokens outside [0, vocab) in
+ * the lists are ignored.  Arrays that are null have no effect (repetition 1, frequency 0, presence 0, no bias, no mask,
+ * prompt_lens 0: all of the history was generated).  Row i's history is history[cu_history[i] .. cu_history[i + 1] - 1], its bias
+ * list likewise, both cut to the lengths given.  Its mask is row mask_rows[i] of `mask` (row i where mask_rows is null); outside
+ * [0, num_masks): no mask.  `out` may be `logits` (same stride); otherwise the two share no element.
+ */
+typedef struct hook_steer_logits_args {
+  int32_t num_rows, vocab, dtype;
+  const void*    logits;           /* [num_rows, vocab], rows logits_stride elements apart (0: vocab) */
+  void*          out;
+  int64_t        logits_stride, out_stride;
+  int32_t        history_len;      /* entries of `history` (0: none, the next two may be null) */
+  const int32_t* history;
+  const int32_t* cu_history;       /* [num_rows + 1] */
+  const int32_t* prompt_lens;      /* [num_rows] or null */
+  const float*   repetition;       /* [num_rows] or null, > 0 */
+  const float*   frequency;        /* [num_rows] or null */
+  const float*   presence;         /* [num_rows] or null */
+  int32_t        bias_len;         /* entries of bias_ids and bias_values (0: none, all three may be null) */
+  const int32_t* cu_bias;          /* [num_rows + 1] */
+  const int32_t* bias_ids;
+  const float*   bias_values;
+  int32_t        num_masks;
+  const uint32_t* mask;            /* [num_masks, ceil(vocab / 32)] or null; bit t % 32 of word t / 32: 1 = allowed */
+  const int32_t* mask_rows;        /* [num_rows] or null */
+  void*          stream;
+} hook_steer_logits_args;
+
+hook_status hook_steer_logits(const hook_steer_logits_args* args);
+
+/*
  * Host helper: parses the layer/heads string of the paper's worker configuration
  * (Section 2.1, `_parse_layer_heads`: '0:0,3,6;15:2' means layer 0 heads 0, 3, 6 and layer 15
  * head 2) into (layer, head) pairs in the order written.  All pointers are HOST pointers.

@@ -15,7 +15,7 @@ LIB = os.path.join(_HERE, "libhook.so")
 BENCH_LIB = os.path.join(_HERE, "libhook_bench.so")
 SOURCES = ["api.hip", "plan.hip", "prefill.hip", "mixed.hip", "decode.hip", "attn_f32.hip", "steer.hip",
            "capture.hip", "reduce.hip", "residual_steer.hip", "span_mass.hip", "config_json.hip", "kv_write.hip",
-           "validate.hip"]
+           "validate.hip", "rope.hip", "pages.hip", "logits.hip"]
 BENCH_SOURCES = ["bench.hip"]
 # packed fp32 instructions are switched off for every device translation unit
 # only what the two headers declare is exported
