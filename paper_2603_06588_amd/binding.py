@@ -514,52 +514,38 @@ def hook_steer(hidden: torch.Tensor, vec: torch.Tensor, alpha: float, token_mask
     return hidden
 
 
-def _launch(fn, args, device, stream, where: str) -> None:
-    """Launches on `device`, which need not be the current one."""
-    if device.index == torch._C._cuda_getDevice():
+# The calls below run on small tensors too, where the host's time is what a call costs: all tensors of a call are looked at in one go
+# (csrc/tensors.cpp: same GPU, types, layouts; an address and sizes for each), and the struct is filled in another.
+
+_look_fn = None
+
+
+def _look(where: str, like, spec, *tensors):
+    global _look_fn
+    if _look_fn is None:
+        if not os.path.exists(os.path.join(_HERE, "_tensors.so")):
+            raise RuntimeError(f"{_HERE}/_tensors.so is missing: build it with `python -m paper_2603_06588_amd.build`")
+        from . import _tensors
+        _tensors.set_error(HookError)
+        _look_fn = _tensors.look
+    return _look_fn(where, like, spec, *tensors)
+
+
+def _launch(fn, args, index: int, stream, where: str) -> None:
+    """Launches on GPU `index`, which need not be the current one."""
+    if index == torch._C._cuda_getDevice():
         args.stream = _stream_handle(stream)
         st = fn(args)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             args.stream = _stream_handle(stream)
             st = fn(args)
     if st != HOOK_OK:
         raise HookError(st, where)
 
 
-def _check(where: str, device, dtype, **tensors) -> None:
-    """Optional contiguous tensors of one type on one GPU."""
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if t.dtype is not dtype:
-            raise HookError(3, f"{where} ({name}: dtype)")
-        if t.device != device:
-            raise HookError(3, f"{where} ({name}: device)")
-        if not t.is_contiguous():
-            raise HookError(2, f"{where} ({name}: layout)")
-
-
-def _on_gpu(where: str, t) -> torch.device:
-    if t.device.type != "cuda":
-        raise HookError(3, f"{where} (device)")
-    return t.device
-
-
-def _row_stride(where: str, name: str, t, device, dtype) -> int:
-    """Elements between the rows of a [rows, ..] tensor whose rows are contiguous."""
-    if t.dtype is not dtype:
-        raise HookError(3, f"{where} ({name}: dtype)")
-    if t.device != device:
-        raise HookError(3, f"{where} ({name}: device)")
-    row = 1
-    for i in range(t.dim() - 1, 0, -1):
-        if t.shape[i] != 1 and t.stride(i) != row:
-            raise HookError(2, f"{where} ({name}: layout)")
-        row *= t.shape[i]
-    if t.shape[0] > 1 and t.stride(0) < row:      # rows on top of each other
-        raise HookError(2, f"{where} ({name}: layout)")
-    return t.stride(0) if t.shape[0] > 1 else row
+_ROPE = ("rq", "rk", "rv", "rq_out", "rk_out", "ipositions", "finv_freq", "cblock_table", "iseq_lens", "icu_q_lens", "ck_cache", "cv_cache", "fk_scale",
+         "fv_scale")
 
 
 def hook_rope(q, k, positions, inv_freq, axis_pairs=None, layout: int = ROPE_HALVES, axis_order: int = ROPE_BLOCKED,
@@ -569,117 +555,109 @@ def hook_rope(q, k, positions, inv_freq, axis_pairs=None, layout: int = ROPE_HAL
     head turn); either may be None.  In place where no output is given.  With k_cache and v_cache the turned keys and v also
     go to the cache, as by ``hook_kv_write``; k itself is then left alone unless it is k_out.  Rows may be views into a wider
     buffer.  Returns (q_out, k_out)."""
-    lib = load_library()
-    first = q if q is not None else k
-    if first is None:
-        raise HookError(1, "hook_rope")
-    dev, dt = _on_gpu("hook_rope", first), first.dtype
+    where = "hook_rope"
+    cached = k_cache is not None or v_cache is not None
+    if q_out is None:
+        q_out = q
+    if k_out is None and not cached:
+        k_out = k
+    like = q if q is not None else k
+    (index, qp, qs, qn, kp, ks, kn, vp, vs, vn, qop, qos, qon, kop, kos, kon, pos, npos, freq, pairs, table, tn, lens, nlens, cu, ncu, kc, kcn, vc, vcn,
+     ksc, nks, vsc, nvs) = _look(where, like, _ROPE, q, k, v, q_out, k_out, positions, inv_freq, block_table, seq_lens, cu_q_lens, k_cache, v_cache,
+                                 k_scale, v_scale)
+    dt = like.dtype
     if dt not in _DT:
         raise HookError(3, "hook_rope (dtype)")
-    a = HookRopeArgs()
-    T, _, d = first.shape
-    _check("hook_rope", dev, torch.int32, positions=positions)
-    _check("hook_rope", dev, torch.float32, inv_freq=inv_freq)
+    shape = qn or kn
+    if len(shape) != 3 or (kn and (len(kn) != 3 or kn[0] != shape[0] or kn[2] != shape[2])):
+        raise HookError(2, "hook_rope (q, k: shape)")
+    T, _, d = shape
+    if qon != qn or (kon and kon != kn):
+        raise HookError(2, "hook_rope (q_out, k_out: shape)")
     axes = positions.shape[0] if positions.dim() == 2 else 1
-    pairs = inv_freq.numel()
-    if positions.numel() != axes * T:
+    if npos != axes * T:
         raise HookError(2, "hook_rope (positions: shape)")
     if axis_pairs is None:
-        if axes != 1:
-            raise HookError(2, "hook_rope (axis_pairs)")
         axis_pairs = (pairs,)
     if len(axis_pairs) != axes or axes > 4:
         raise HookError(2, "hook_rope (axis_pairs)")
-    a.num_tokens, a.head_dim, a.rotary_dim, a.num_axes = T, d, 2 * pairs, axes
-    for i in range(axes):
-        a.axis_pairs[i] = axis_pairs[i]
-    a.layout, a.axis_order, a.inverse, a.dtype, a.magnitude = layout, axis_order, bool(inverse), _DT[dt], magnitude
-    a.positions, a.inv_freq = _p(positions), _p(inv_freq)
-    cached = k_cache is not None or v_cache is not None
-    if q is not None:
-        q_out = q if q_out is None else q_out
-        if q_out.shape != q.shape:
-            raise HookError(2, "hook_rope (q_out: shape)")
-        a.num_q_heads = q.shape[1]
-        a.q, a.q_stride = _p(q), _row_stride("hook_rope", "q", q, dev, dt)
-        a.q_out, a.q_out_stride = _p(q_out), _row_stride("hook_rope", "q_out", q_out, dev, dt)
-    if k is not None:
-        if k.shape[0] != T or k.shape[2] != d:
-            raise HookError(2, "hook_rope (k: shape)")
-        if k_out is None and not cached:
-            k_out = k
-        a.num_kv_heads = k.shape[1]
-        a.k, a.k_stride = _p(k), _row_stride("hook_rope", "k", k, dev, dt)
-        if k_out is not None:
-            if k_out.shape != k.shape:
-                raise HookError(2, "hook_rope (k_out: shape)")
-            a.k_out, a.k_out_stride = _p(k_out), _row_stride("hook_rope", "k_out", k_out, dev, dt)
+    a = HookRopeArgs(T, qn[1] if qn else 0, kn[1] if kn else 0, d, 2 * pairs, axes, (ctypes.c_int32 * 4)(*axis_pairs), layout, axis_order,
+                     1 if inverse else 0, _DT[dt], magnitude, pos, freq, qp, kp, qop, kop, qs, ks, qos, kos)
     if cached:
-        if k is None or v is None or k_cache is None or v_cache is None or block_table is None or seq_lens is None or cu_q_lens is None:
+        if not kn or v is None or k_cache is None or v_cache is None or block_table is None or seq_lens is None or cu_q_lens is None:
             raise HookError(1, "hook_rope (cache)")
-        if v.shape != k.shape:
-            raise HookError(2, "hook_rope (v: shape)")
-        kv8 = k_cache.dtype == torch.uint8
-        _check("hook_rope", dev, torch.uint8 if kv8 else dt, k_cache=k_cache, v_cache=v_cache)
-        _check("hook_rope", dev, torch.int32, block_table=block_table, seq_lens=seq_lens, cu_q_lens=cu_q_lens)
-        _check("hook_rope", dev, torch.float32, k_scale=k_scale, v_scale=v_scale)
-        num_blocks, Hkv, B, dc = k_cache.shape
-        num_seqs, max_blocks = block_table.shape
-        if (Hkv, dc) != (k.shape[1], d) or v_cache.shape != k_cache.shape or seq_lens.numel() != num_seqs or cu_q_lens.numel() != num_seqs + 1:
-            raise HookError(2, "hook_rope (cache: shape)")
-        if kv8 and any(s is not None and s.numel() != Hkv for s in (k_scale, v_scale)):
-            raise HookError(2, "hook_rope (k_scale, v_scale: shape)")
-        a.num_seqs, a.block_size, a.max_blocks_per_seq, a.num_blocks = num_seqs, B, max_blocks, num_blocks
-        a.v, a.v_stride = _p(v), _row_stride("hook_rope", "v", v, dev, dt)
-        a.block_table, a.seq_lens, a.cu_q_lens = _p(block_table), _p(seq_lens), _p(cu_q_lens)
-        a.k_cache, a.v_cache = _p(k_cache), _p(v_cache)
-        if kv8:
-            a.kv_dtype, a.k_scale, a.v_scale = KV_FP8_E4M3, _p(k_scale), _p(v_scale)
-    _launch(lib.hook_rope, a, dev, stream, "hook_rope")
+        if len(kcn) != 4 or kcn[1] != kn[1] or kcn[3] != d or vcn != kcn or vn != kn:
+            raise HookError(2, "hook_rope (v, k_cache, v_cache: shape)")
+        if len(tn) != 2 or nlens != tn[0] or ncu != nlens + 1:
+            raise HookError(2, "hook_rope (block_table, seq_lens, cu_q_lens: shape)")
+        kind = k_cache.dtype
+        if v_cache.dtype is not kind or block_table.dtype is not torch.int32:
+            raise HookError(3, "hook_rope (v_cache, block_table: dtype)")
+        a.num_seqs, a.block_size, a.max_blocks_per_seq, a.num_blocks = tn[0], kcn[2], tn[1], kcn[0]
+        a.v, a.v_stride, a.block_table, a.seq_lens, a.cu_q_lens, a.k_cache, a.v_cache = vp, vs, table, lens, cu, kc, vc
+        if kind is torch.uint8:       # 8-bit E4M3 bytes with one scale per kv head
+            if nks != kn[1] or nvs != kn[1]:
+                raise HookError(2, "hook_rope (k_scale, v_scale: shape)")
+            a.kv_dtype, a.k_scale, a.v_scale = KV_FP8_E4M3, ksc, vsc
+        elif kind is not dt:
+            raise HookError(3, "hook_rope (k_cache: dtype)")
+    _launch((_lib or load_library()).hook_rope, a, index, stream, where)
     return q_out, k_out
 
 
-def _pages_args(where: str, block_table, seq_lens, ref_counts, status, **more) -> "HookPagesArgs":
-    dev = _on_gpu(where, block_table)
-    _check(where, dev, torch.int32, block_table=block_table, seq_lens=seq_lens, ref_counts=ref_counts, status=status, **more)
-    a = HookPagesArgs()
-    a.num_seqs, a.max_blocks_per_seq = block_table.shape
-    a.num_blocks, a.block_size = ref_counts.numel(), 16
-    if seq_lens.numel() != a.num_seqs or status.numel() != 1:
-        raise HookError(2, f"{where} (seq_lens, status: shape)")
-    a.block_table, a.seq_lens, a.ref_counts, a.status = _p(block_table), _p(seq_lens), _p(ref_counts), _p(status)
-    return a
+_PAGES = ("iblock_table", "iseq_lens", "iref_counts", "iblock_table_out", "iseq_lens_out", "iref_counts_out", "istatus", "isrc_rows", "isrc_lens",
+          "icu_q_lens", "ipage_map", "inum_live")
 
 
-def _pages_data(where: str, lib, a, caches, workspace, device, stream):
+def _pages_args(where: str, block_table, seq_lens, ref_counts, table_out, lens_out, refs_out, status, src_rows=None, src_lens=None, cu_q_lens=None,
+                page_map=None, num_live=None):
+    """(struct without the data, index of the GPU); an output that is None is its input."""
+    (index, table, _, lens, nlens, refs, num_blocks, to, nto, lens_to, nlens_to, refs_to, nrefs, st, nst, src, rows, cut, ncut, cu, ncu, pm, npm, live,
+     nlive) = _look(where, block_table, _PAGES, block_table, seq_lens, ref_counts, block_table if table_out is None else table_out,
+                    seq_lens if lens_out is None else lens_out, ref_counts if refs_out is None else refs_out, status, src_rows, src_lens, cu_q_lens,
+                    page_map, num_live)
+    if block_table.dim() != 2:
+        raise HookError(2, f"{where} (block_table: shape)")
+    num_seqs, max_blocks = block_table.shape
+    new_rows = num_seqs if src_rows is None else rows
+    if (nlens != num_seqs or nst != 1 or nrefs != num_blocks or nto != new_rows * max_blocks or nlens_to != new_rows or
+            (src_lens is not None and ncut != rows) or (cu_q_lens is not None and ncu != num_seqs + 1) or
+            (page_map is not None and (npm != num_blocks or nlive != 1))):
+        raise HookError(2, f"{where} (shape)")
+    return HookPagesArgs(num_seqs, max_blocks, num_blocks, 16, table, lens, refs, to, lens_to, refs_to, st, rows, src, cut, cu, pm, live), index
+
+
+_CACHES: dict = {}      # "caches[0]", "caches[1]", ... as often as the longest list so far
+
+
+def _pages_data(where: str, lib, a, caches, like, workspace, index: int, stream):
     """Fills in the caches (a list of [num_blocks, Hkv, 16, d] tensors, or one tensor of them stacked) and the scratch; returns
     what has to live until the call has returned."""
-    if not isinstance(caches, torch.Tensor):
-        caches = list(caches)
-        pointers = [c.data_ptr() for c in caches]
-        each = caches
-    else:
-        step = caches.stride(0) * caches.element_size()
-        pointers = [caches.data_ptr() + i * step for i in range(caches.shape[0])]
-        each = [caches[0]] if pointers else []
-    for c in each:
-        if c.device != device:
-            raise HookError(3, f"{where} (caches: device)")
-        if not c.is_contiguous():
-            raise HookError(2, f"{where} (caches: layout)")
-        if c.dim() != 4 or c.shape[0] != a.num_blocks or c.shape[2] != 16 or c.shape != each[0].shape or c.dtype != each[0].dtype:
-            raise HookError(2, f"{where} (caches: shape)")
-    array = (ctypes.c_void_p * max(len(pointers), 1))(*pointers)
-    a.num_caches, a.caches = len(pointers), array
-    if each:
-        a.num_kv_heads, a.row_bytes = each[0].shape[1], each[0].shape[3] * each[0].element_size()
+    stacked = isinstance(caches, torch.Tensor)
+    each = (caches,) if stacked else tuple(caches)
+    n = len(each)
+    spec = _CACHES.get(n)
+    if spec is None:
+        spec = _CACHES[n] = tuple(f"ccaches[{i}]" for i in range(n)) + ("cworkspace",)
     if workspace is None:
-        workspace = torch.empty(lib.hook_pages_workspace_bytes(a), dtype=torch.uint8, device=device)
+        workspace = torch.empty(lib.hook_pages_workspace_bytes(a), dtype=torch.uint8, device=index)
         if stream is not None:
             workspace.record_stream(stream)
-    elif workspace.device != device or not workspace.is_contiguous():
-        raise HookError(4, f"{where} (workspace)")
-    a.workspace, a.workspace_bytes = _p(workspace), workspace.numel() * workspace.element_size()
+    seen = _look(where, like, spec, *each, workspace)
+    a.workspace, a.workspace_bytes = seen[-2], workspace.numel() * workspace.element_size()
+    pointers = seen[1:-2:2]
+    if n:
+        shape, dtype = seen[2], each[0].dtype
+        if len(shape) != (5 if stacked else 4) or shape[-4] != a.num_blocks or shape[-2] != 16:
+            raise HookError(2, f"{where} (caches: shape)")
+        if n > 1 and any(s != shape for s in seen[4:-2:2]) or any(c.dtype is not dtype for c in each):
+            raise HookError(2, f"{where} (caches: shape, dtype)")
+        a.num_kv_heads, a.row_bytes = shape[-3], shape[-1] * each[0].element_size()
+        if stacked:
+            n, step = shape[0], shape[1] * shape[2] * 16 * a.row_bytes
+            pointers = range(pointers[0], pointers[0] + n * step, step) if n else ()
+    array = (ctypes.c_void_p * (n or 1))(*pointers)
+    a.num_caches, a.caches = n, array
     return array, workspace
 
 
@@ -695,36 +673,19 @@ def hook_pages_fork(src_rows, block_table, seq_lens, ref_counts, block_table_out
     """Replaces a block table by block_table_out / seq_lens_out, whose row j takes the first src_lens[j] (None: all) tokens of row
     src_rows[j], or is empty where that is -1; reference counts follow (in place unless ref_counts_out is given).  Bits of PAGES_* are
     added to `status`."""
-    lib = load_library()
-    refs_out = ref_counts if ref_counts_out is None else ref_counts_out
-    a = _pages_args("hook_pages_fork", block_table, seq_lens, ref_counts, status, src_rows=src_rows, src_lens=src_lens,
-                    block_table_out=block_table_out, seq_lens_out=seq_lens_out, ref_counts_out=refs_out)
-    rows = src_rows.numel()
-    if (tuple(block_table_out.shape) != (rows, a.max_blocks_per_seq) or seq_lens_out.numel() != rows or refs_out.numel() != a.num_blocks or
-            (src_lens is not None and src_lens.numel() != rows)):
-        raise HookError(2, "hook_pages_fork (shape)")
-    a.num_rows, a.src_rows, a.src_lens = rows, _p(src_rows), _p(src_lens)
-    a.block_table_out, a.seq_lens_out, a.ref_counts_out = _p(block_table_out), _p(seq_lens_out), _p(refs_out)
-    _launch(lib.hook_pages_fork, a, block_table.device, stream, "hook_pages_fork")
+    where = "hook_pages_fork"
+    a, index = _pages_args(where, block_table, seq_lens, ref_counts, block_table_out, seq_lens_out, ref_counts_out, status, src_rows, src_lens)
+    _launch((_lib or load_library()).hook_pages_fork, a, index, stream, where)
 
 
 def hook_pages_append(cu_q_lens, block_table, seq_lens, ref_counts, caches, status, block_table_out=None, seq_lens_out=None,
                       ref_counts_out=None, workspace=None, stream=None):
     """Room for the new tokens of each row: lengths grow, pages are taken, last pages that others hold too are copied in every
     cache.  In place unless outputs are given; all or nothing (PAGES_FULL in `status`)."""
-    lib = load_library()
-    table_out = block_table if block_table_out is None else block_table_out
-    lens_out = seq_lens if seq_lens_out is None else seq_lens_out
-    refs_out = ref_counts if ref_counts_out is None else ref_counts_out
-    a = _pages_args("hook_pages_append", block_table, seq_lens, ref_counts, status, cu_q_lens=cu_q_lens, block_table_out=table_out,
-                    seq_lens_out=lens_out, ref_counts_out=refs_out)
-    if (table_out.shape != block_table.shape or lens_out.numel() != a.num_seqs or refs_out.numel() != a.num_blocks or
-            cu_q_lens.numel() != a.num_seqs + 1):
-        raise HookError(2, "hook_pages_append (shape)")
-    a.cu_q_lens = _p(cu_q_lens)
-    a.block_table_out, a.seq_lens_out, a.ref_counts_out = _p(table_out), _p(lens_out), _p(refs_out)
-    keep = _pages_data("hook_pages_append", lib, a, caches, workspace, block_table.device, stream)
-    _launch(lib.hook_pages_append, a, block_table.device, stream, "hook_pages_append")
+    where, lib = "hook_pages_append", _lib or load_library()
+    a, index = _pages_args(where, block_table, seq_lens, ref_counts, block_table_out, seq_lens_out, ref_counts_out, status, cu_q_lens=cu_q_lens)
+    keep = _pages_data(where, lib, a, caches, block_table, workspace, index, stream)
+    _launch(lib.hook_pages_append, a, index, stream, where)
     del keep
 
 
@@ -732,52 +693,36 @@ def hook_pages_compact(block_table, seq_lens, ref_counts, caches, page_map, num_
                        ref_counts_out=None, workspace=None, stream=None):
     """Moves the live pages to the front of every cache and renumbers the table and the counts (in place unless outputs are
     given); page_map receives every page's new number (-1: free), num_live how many there are."""
-    lib = load_library()
-    table_out = block_table if block_table_out is None else block_table_out
-    refs_out = ref_counts if ref_counts_out is None else ref_counts_out
-    a = _pages_args("hook_pages_compact", block_table, seq_lens, ref_counts, status, page_map=page_map, num_live=num_live,
-                    block_table_out=table_out, ref_counts_out=refs_out)
-    if table_out.shape != block_table.shape or refs_out.numel() != a.num_blocks or page_map.numel() != a.num_blocks or num_live.numel() != 1:
-        raise HookError(2, "hook_pages_compact (shape)")
-    a.block_table_out, a.ref_counts_out, a.page_map, a.num_live = _p(table_out), _p(refs_out), _p(page_map), _p(num_live)
-    keep = _pages_data("hook_pages_compact", lib, a, caches, workspace, block_table.device, stream)
-    _launch(lib.hook_pages_compact, a, block_table.device, stream, "hook_pages_compact")
+    where, lib = "hook_pages_compact", _lib or load_library()
+    a, index = _pages_args(where, block_table, seq_lens, ref_counts, block_table_out, None, ref_counts_out, status, page_map=page_map, num_live=num_live)
+    keep = _pages_data(where, lib, a, caches, block_table, workspace, index, stream)
+    _launch(lib.hook_pages_compact, a, index, stream, where)
     del keep
+
+
+_LOGITS = ("rlogits", "rout", "ihistory", "icu_history", "iprompt_lens", "frepetition", "ffrequency", "fpresence", "icu_bias", "ibias_ids",
+           "fbias_values", "imask", "imask_rows")
 
 
 def hook_steer_logits(logits, out=None, history=None, cu_history=None, prompt_lens=None, repetition=None, frequency=None,
                       presence=None, cu_bias=None, bias_ids=None, bias_values=None, mask=None, mask_rows=None, stream=None):
     """Penalties for repeated tokens, a bias list and a grammar mask (int32 words, a set bit allows its token) on logits [rows, vocab], in
     place unless `out` is given.  Lists are int32 with prefix sums cu_*.  Returns the result."""
-    lib = load_library()
-    dev, dt = _on_gpu("hook_steer_logits", logits), logits.dtype
-    if dt not in _DT or logits.dim() != 2:
+    where = "hook_steer_logits"
+    if out is None:
+        out = logits
+    (index, x, xs, xn, y, ys, yn, h, nh, cuh, ncuh, pl, npl, rep, nrep, fr, nfr, pr, npr, cub, ncub, bi, nbi, bv, nbv, m, nm, mr,
+     nmr) = _look(where, logits, _LOGITS, logits, out, history, cu_history, prompt_lens, repetition, frequency, presence, cu_bias, bias_ids,
+                  bias_values, mask, mask_rows)
+    dt = logits.dtype
+    if dt not in _DT or len(xn) != 2:
         raise HookError(3, "hook_steer_logits (dtype)")
-    out = logits if out is None else out
-    rows, vocab = logits.shape
-    if out.shape != logits.shape:
-        raise HookError(2, "hook_steer_logits (out: shape)")
-    _check("hook_steer_logits", dev, torch.int32, history=history, cu_history=cu_history, prompt_lens=prompt_lens, cu_bias=cu_bias,
-           bias_ids=bias_ids, mask=mask, mask_rows=mask_rows)
-    _check("hook_steer_logits", dev, torch.float32, repetition=repetition, frequency=frequency, presence=presence, bias_values=bias_values)
-    for t, n in ((prompt_lens, rows), (repetition, rows), (frequency, rows), (presence, rows), (mask_rows, rows), (cu_history, rows + 1),
-                 (cu_bias, rows + 1)):
-        if t is not None and t.numel() != n:
-            raise HookError(2, "hook_steer_logits (shape)")
-    a = HookSteerLogitsArgs()
-    a.num_rows, a.vocab, a.dtype = rows, vocab, _DT[dt]
-    a.logits, a.logits_stride = _p(logits), _row_stride("hook_steer_logits", "logits", logits, dev, dt)
-    a.out, a.out_stride = _p(out), _row_stride("hook_steer_logits", "out", out, dev, dt)
-    if history is not None:
-        a.history_len, a.history, a.cu_history, a.prompt_lens = history.numel(), _p(history), _p(cu_history), _p(prompt_lens)
-    a.repetition, a.frequency, a.presence = _p(repetition), _p(frequency), _p(presence)
-    if bias_ids is not None:
-        if bias_values is None or bias_values.numel() != bias_ids.numel():
-            raise HookError(2, "hook_steer_logits (bias: shape)")
-        a.bias_len, a.cu_bias, a.bias_ids, a.bias_values = bias_ids.numel(), _p(cu_bias), _p(bias_ids), _p(bias_values)
-    if mask is not None:
-        if mask.dim() != 2 or mask.shape[1] != (vocab + 31) // 32:
-            raise HookError(2, "hook_steer_logits (mask: shape)")
-        a.num_masks, a.mask, a.mask_rows = mask.shape[0], _p(mask), _p(mask_rows)
-    _launch(lib.hook_steer_logits, a, dev, stream, "hook_steer_logits")
+    rows, vocab = xn
+    words = (vocab + 31) // 32
+    if (yn != xn or (cu_history is not None and ncuh != rows + 1) or (prompt_lens is not None and npl != rows) or (repetition is not None and nrep != rows) or
+            (frequency is not None and nfr != rows) or (presence is not None and npr != rows) or (cu_bias is not None and ncub != rows + 1) or nbi != nbv or
+            (mask_rows is not None and nmr != rows) or (mask is not None and (mask.dim() != 2 or mask.shape[1] != words))):
+        raise HookError(2, "hook_steer_logits (shape)")
+    a = HookSteerLogitsArgs(rows, vocab, _DT[dt], x, y, xs, ys, nh, h, cuh, pl, rep, fr, pr, nbi, cub, bi, bv, nm // words if words else 0, m, mr)
+    _launch((_lib or load_library()).hook_steer_logits, a, index, stream, where)
     return out
