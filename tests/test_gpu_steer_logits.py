@@ -124,6 +124,47 @@ def test_padded_and_misaligned_rows(dtype, stride, offset):
     assert torch.equal(bits(wide[pad]), bits(before[pad]))       # what lies between and around the rows
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("shift_in,shift_out,stride", [(0, 0, 1003), (3, 3, 1000), (1, 2, 1000), (0, 4, 1008), (5, 5, 1001)])
+def test_rows_off_the_borders_of_16_bytes(dtype, shift_in, shift_out, stride):
+    """Input and output rows that begin anywhere, alike or not, with masks that begin inside a word for them."""
+    c = Case(9, 997, dtype, seed=shift_in + stride, bias=6, masks=4)
+    a = torch.zeros(shift_in + 9 * stride, dtype=dtype, device=DEV)
+    b = torch.full((shift_out + 9 * stride,), 2.0, dtype=dtype, device=DEV)
+    x, y = a[shift_in:].view(9, stride)[:, :997], b[shift_out:].view(9, stride)[:, :997]
+    x.copy_(c.logits)
+    binding.hook_steer_logits(x, out=y, **c.kwargs())
+    c.check(y)
+    pad = torch.ones_like(b, dtype=torch.bool)
+    pad[shift_out:].view(9, stride)[:, :997] = False
+    assert bool((b[pad] == 2.0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_more_touched_tokens_than_are_listed(dtype):
+    # nearly every token of a range occurs, and a bias list longer than a workgroup, with tokens named over and over
+    c = Case(2, 20000, dtype, seed=4, hist=30000, bias=3000)
+    c.history[1] = list(range(0, 20000, 2)) + [3] * 50
+    c.prompt[1] = 7000
+    out = torch.empty((2, 20000), dtype=dtype, device=DEV)
+    binding.hook_steer_logits(c.logits.to(DEV), out=out, **c.kwargs())
+    c.check(out)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_counts_beyond_16_bits(dtype):
+    # 70000 generated tokens: one of them 40000 times, the rest spread over both halves of the range
+    V = 17000
+    h = [[5] * 100 + [16500] * 40000 + [t % V for t in range(30000)], [3, 16999]]
+    c = Case(2, V, F32, seed=5, bias=40)
+    c.logits = c.logits.to(dtype)
+    c.history, c.prompt = h, [100, 1]
+    c.rep, c.freq, c.pres = torch.tensor([1.5, 1.25]), torch.tensor([2.0 ** -10, 0.5]), torch.tensor([0.25, 0.75])
+    out = torch.empty((2, V), dtype=dtype, device=DEV)
+    binding.hook_steer_logits(c.logits.to(DEV), out=out, **c.kwargs())
+    c.check(out)
+
+
 def test_long_history_and_counts():
     # one token 20000 times, half of them in the prompt: 10000 * 0.125 is exact
     x = torch.zeros((1, 40000), device=DEV)
