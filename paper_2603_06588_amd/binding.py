@@ -8,6 +8,7 @@ built (``python -m paper_2603_06588_amd.build``).
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Tuple
 
@@ -544,6 +545,7 @@ def _launch(fn, args, index: int, stream, where: str) -> None:
         raise HookError(st, where)
 
 
+_FourInts = ctypes.c_int32 * 4
 _ROPE = ("rq", "rk", "rv", "rq_out", "rk_out", "ipositions", "finv_freq", "cblock_table", "iseq_lens", "icu_q_lens", "ck_cache", "cv_cache", "fk_scale",
          "fv_scale")
 
@@ -581,8 +583,7 @@ def hook_rope(q, k, positions, inv_freq, axis_pairs=None, layout: int = ROPE_HAL
         axis_pairs = (pairs,)
     if len(axis_pairs) != axes or axes > 4:
         raise HookError(2, "hook_rope (axis_pairs)")
-    a = HookRopeArgs(T, qn[1] if qn else 0, kn[1] if kn else 0, d, 2 * pairs, axes, (ctypes.c_int32 * 4)(*axis_pairs), layout, axis_order,
-                     1 if inverse else 0, _DT[dt], magnitude, pos, freq, qp, kp, qop, kop, qs, ks, qos, kos)
+    kv_dtype = num_seqs = block_size = max_blocks = num_blocks = 0
     if cached:
         if not kn or v is None or k_cache is None or v_cache is None or block_table is None or seq_lens is None or cu_q_lens is None:
             raise HookError(1, "hook_rope (cache)")
@@ -593,14 +594,18 @@ def hook_rope(q, k, positions, inv_freq, axis_pairs=None, layout: int = ROPE_HAL
         kind = k_cache.dtype
         if v_cache.dtype is not kind or block_table.dtype is not torch.int32:
             raise HookError(3, "hook_rope (v_cache, block_table: dtype)")
-        a.num_seqs, a.block_size, a.max_blocks_per_seq, a.num_blocks = tn[0], kcn[2], tn[1], kcn[0]
-        a.v, a.v_stride, a.block_table, a.seq_lens, a.cu_q_lens, a.k_cache, a.v_cache = vp, vs, table, lens, cu, kc, vc
         if kind is torch.uint8:       # 8-bit E4M3 bytes with one scale per kv head
             if nks != kn[1] or nvs != kn[1]:
                 raise HookError(2, "hook_rope (k_scale, v_scale: shape)")
-            a.kv_dtype, a.k_scale, a.v_scale = KV_FP8_E4M3, ksc, vsc
+            kv_dtype = KV_FP8_E4M3
         elif kind is not dt:
             raise HookError(3, "hook_rope (k_cache: dtype)")
+        num_seqs, max_blocks, num_blocks, block_size = nlens, tn[1], kcn[0], kcn[2]
+    else:
+        vp = table = lens = cu = 0
+    a = HookRopeArgs(T, qn[1] if qn else 0, kn[1] if kn else 0, d, 2 * pairs, axes, _FourInts(*axis_pairs), layout, axis_order, 1 if inverse else 0,
+                     _DT[dt], magnitude, pos, freq, qp, kp, qop, kop, qs, ks, qos, kos, num_seqs, block_size, max_blocks, num_blocks, vp, vs, table,
+                     lens, cu, kc, vc, kv_dtype, ksc, vsc)
     _launch((_lib or load_library()).hook_rope, a, index, stream, where)
     return q_out, k_out
 
@@ -630,7 +635,7 @@ def _pages_args(where: str, block_table, seq_lens, ref_counts, table_out, lens_o
 _CACHES: dict = {}      # "caches[0]", "caches[1]", ... as often as the longest list so far
 
 
-def _pages_data(where: str, lib, a, caches, like, workspace, index: int, stream):
+def _pages_data(where: str, a, caches, like, workspace, index: int, stream):
     """Fills in the caches (a list of [num_blocks, Hkv, 16, d] tensors, or one tensor of them stacked) and the scratch; returns
     what has to live until the call has returned."""
     stacked = isinstance(caches, torch.Tensor)
@@ -640,7 +645,7 @@ def _pages_data(where: str, lib, a, caches, like, workspace, index: int, stream)
     if spec is None:
         spec = _CACHES[n] = tuple(f"ccaches[{i}]" for i in range(n)) + ("cworkspace",)
     if workspace is None:
-        workspace = torch.empty(lib.hook_pages_workspace_bytes(a), dtype=torch.uint8, device=index)
+        workspace = torch.empty(pages_workspace_bytes(a.num_seqs, a.num_blocks), dtype=torch.uint8, device=index)
         if stream is not None:
             workspace.record_stream(stream)
     seen = _look(where, like, spec, *each, workspace)
@@ -661,6 +666,7 @@ def _pages_data(where: str, lib, a, caches, like, workspace, index: int, stream)
     return array, workspace
 
 
+@functools.lru_cache(maxsize=64)
 def pages_workspace_bytes(num_seqs: int, num_blocks: int) -> int:
     """Scratch bytes of ``hook_pages_append`` and ``hook_pages_compact``."""
     a = HookPagesArgs()
@@ -682,10 +688,10 @@ def hook_pages_append(cu_q_lens, block_table, seq_lens, ref_counts, caches, stat
                       ref_counts_out=None, workspace=None, stream=None):
     """Room for the new tokens of each row: lengths grow, pages are taken, last pages that others hold too are copied in every
     cache.  In place unless outputs are given; all or nothing (PAGES_FULL in `status`)."""
-    where, lib = "hook_pages_append", _lib or load_library()
+    where = "hook_pages_append"
     a, index = _pages_args(where, block_table, seq_lens, ref_counts, block_table_out, seq_lens_out, ref_counts_out, status, cu_q_lens=cu_q_lens)
-    keep = _pages_data(where, lib, a, caches, block_table, workspace, index, stream)
-    _launch(lib.hook_pages_append, a, index, stream, where)
+    keep = _pages_data(where, a, caches, block_table, workspace, index, stream)
+    _launch((_lib or load_library()).hook_pages_append, a, index, stream, where)
     del keep
 
 
@@ -693,10 +699,10 @@ def hook_pages_compact(block_table, seq_lens, ref_counts, caches, page_map, num_
                        ref_counts_out=None, workspace=None, stream=None):
     """Moves the live pages to the front of every cache and renumbers the table and the counts (in place unless outputs are
     given); page_map receives every page's new number (-1: free), num_live how many there are."""
-    where, lib = "hook_pages_compact", _lib or load_library()
+    where = "hook_pages_compact"
     a, index = _pages_args(where, block_table, seq_lens, ref_counts, block_table_out, None, ref_counts_out, status, page_map=page_map, num_live=num_live)
-    keep = _pages_data(where, lib, a, caches, block_table, workspace, index, stream)
-    _launch(lib.hook_pages_compact, a, index, stream, where)
+    keep = _pages_data(where, a, caches, block_table, workspace, index, stream)
+    _launch((_lib or load_library()).hook_pages_compact, a, index, stream, where)
     del keep
 
 

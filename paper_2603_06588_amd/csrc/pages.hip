@@ -4,8 +4,9 @@
 //
 // Bookkeeping is bound by launches and by trips to memory, the data by its bandwidth: a copied page is read once and
 // written once, by workgroups that take one piece of one page in one cache at a time.
-// Sums over pages (which is the k-th free one) are taken in two steps: a launch counts every chunk of kChunk pages, and each
-// workgroup of the next one adds up the counts before its own chunk for itself, which saves a launch in between.
+// Which page is the k-th free (or live) one is a sum over all pages.  It is taken in two launches: the first lists the free pages of every
+// chunk of kChunk pages and counts them; every workgroup of the second adds the chunks' counts up for itself and then looks a page up
+// by its number.  (A launch in between that hands the pages out made the step after a fork of 512 rows 34 us.)
 #include "../../include/hook_api.h"
 #include "hook_device.h"
 
@@ -19,10 +20,10 @@ constexpr int kRowChunk = 1024;       // table entries of a workgroup, four to a
 constexpr int kTooMany = 0x3fffffff;  // "needs" of a row that the table cannot hold: more than any cache has
 
 struct RowPlan {
-  int need;    // new pages
-  int start;   // first table entry that gets one
+  int start;   // first table entry that gets a new page
   int tail;    // page to be copied into the first of them, or -1
   int len;     // tokens that the row holds before the call
+  int grow;    // tokens that it is to hold more
 };
 
 struct PagesParams {
@@ -33,13 +34,22 @@ struct PagesParams {
   int *page_map, *num_live;
   // scratch
   int nc;            // chunks
-  int* counts;       // [nc] free (append) or live (compact) pages of a chunk
-  RowPlan* plan;     // [S]
-  int *order, *movers, *holes, *moves;
+  int* counts;       // [nc] free pages of a chunk
+  int* free_list;    // [nc, kChunk] the free pages of each chunk
+  int* live_list;    // [nc, kChunk] the live ones (compact)
+  int* order;        // [nb] a live page's number among those of its chunk, or -1 - a free one's (compact)
+  int* need;         // [S] new pages of a row (append)
+  RowPlan* plan;     // [S] (append)
   // data
   int ncaches, heads;
   int row_chunks;    // 16-byte pieces of a token row of one head
-  void* cache[HOOK_PAGES_MAX_CACHES];
+  int keep_lines;    // the caches fit the last-level cache (compact)
+};
+
+// The caches travel as an argument of their own, of two lengths: a launch with 2 KB of arguments costs the host more than one with 256 bytes.
+constexpr int kFewCaches = 32;
+template <int N> struct CacheList {
+  void* cache[N];
 };
 
 // Sum over the workgroup, in every thread; `sh` holds one value per wave.
@@ -152,27 +162,74 @@ __global__ __launch_bounds__(kThreads) void k_pages_fork(const PagesParams p, in
   report(p, bits);
 }
 
-// ---- counting, shared by append and compact ---------------------------------------------------------------
+// ---- the pages by number, for append and compact ----------------------------------------------------------
 
-// Counts of this thread's eight pages; entries past the last page read as `past`.
-__device__ __forceinline__ void chunk_refs(const int* refs, int nb, int chunk, int past, int (&r)[kPer]) {
+// A chunk: its free pages are listed and counted, and for a compaction the live ones too.
+template <bool LIVE>
+__device__ __forceinline__ void list_chunk(const PagesParams& p, int chunk, int* sh) {
+  const int tid = threadIdx.x, first = chunk * kChunk + tid * kPer;
+  int r[kPer], n = 0, count;
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) r[u] = first + u < p.nb ? p.refs[first + u] : 1;
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) n += r[u] <= 0;
+  int frees = block_scan(n, sh, &count), lives = tid * kPer - frees;
 #pragma unroll
   for (int u = 0; u < kPer; ++u) {
-    const int page = chunk * kChunk + threadIdx.x * kPer + u;
-    r[u] = page < nb ? refs[page] : past;
+    if (first + u >= p.nb) break;
+    if (p.refs_out != p.refs) p.refs_out[first + u] = r[u];
+    if (LIVE) p.order[first + u] = r[u] <= 0 ? -1 - frees : lives;
+    if (r[u] <= 0) p.free_list[(size_t)chunk * kChunk + frees++] = first + u;
+    else if (LIVE) p.live_list[(size_t)chunk * kChunk + lives++] = first + u;
+    else ++lives;
   }
+  if (tid == 0) p.counts[chunk] = count;
 }
 
-// Chunk counts before `chunk` and all of them.
-__device__ __forceinline__ long long counts_before(const PagesParams& p, int chunk, long long* sh, long long* all) {
-  long long before = 0, sum = 0;
-  for (int c = threadIdx.x; c < p.nc; c += kThreads) {
-    const int n = p.counts[c];
-    sum += n;
-    if (c < chunk) before += n;
+// What a workgroup knows of all chunks: free pages before every segment of them (one chunk to a segment up to kThreads chunks).
+struct Ranks {
+  int before[kThreads + 1];
+};
+
+__device__ __forceinline__ int chunks_per_segment(const PagesParams& p) { return (p.nc + kThreads - 1) / kThreads; }
+
+__device__ __forceinline__ void load_ranks(const PagesParams& p, Ranks& ranks, int* sh) {
+  const int tid = threadIdx.x, per = chunks_per_segment(p);
+  int n = 0, all;
+  for (int c = tid * per; c < min((tid + 1) * per, p.nc); ++c) n += p.counts[c];
+  ranks.before[tid] = block_scan(n, sh, &all);
+  if (tid == 0) ranks.before[kThreads] = all;
+  __syncthreads();
+}
+
+__device__ __forceinline__ int frees_before(const PagesParams& p, const Ranks& ranks, int chunk) {
+  const int per = chunks_per_segment(p), seg = chunk / per;
+  int n = ranks.before[seg];
+  for (int c = seg * per; c < chunk; ++c) n += p.counts[c];
+  return n;
+}
+
+// The k-th free page, or the k-th live one (0 is the lowest).
+template <bool LIVE>
+__device__ __forceinline__ int page_by_number(const PagesParams& p, const Ranks& ranks, int k) {
+  const int per = chunks_per_segment(p);
+  auto before = [&](int seg) {
+    const int n = ranks.before[seg];
+    return LIVE ? (int)min((long long)seg * per * kChunk, (long long)p.nb) - n : n;
+  };
+  int lo = 0, hi = kThreads;      // the last segment with no more than k before it
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (before(mid) <= k) lo = mid; else hi = mid;
   }
-  *all = block_sum(sum, sh);
-  return block_sum(before, sh);
+  int c = lo * per;
+  k -= before(lo);
+  for (; per > 1 && c + 1 < p.nc; ++c) {
+    const int n = LIVE ? kChunk - p.counts[c] : p.counts[c];
+    if (k < n) break;
+    k -= n;
+  }
+  return (LIVE ? p.live_list : p.free_list)[(size_t)c * kChunk + k];
 }
 
 // ---- append ---------------------------------------------------------------------------------------------
@@ -188,21 +245,13 @@ __device__ __forceinline__ bool appends(const PagesParams& p, int i, int* len, i
 
 __device__ __forceinline__ int last_page(const PagesParams& p, int i, int len) { return p.table[(size_t)i * p.mb + len / kBlock]; }
 
-// Workgroups below nc count the free pages of a chunk; in the others a wave plans a row: it looks through the rows before its own
-// for those that leave the same last page.
+// Workgroups below nc list the free pages of a chunk; in the others a wave plans a row: it looks through the rows before its own
+// for those that leave the same last page, kRowsAhead rows to a lane at a time (one at a time, 512 rows took eight times two trips
+// to memory one after the other: 8.0 us instead of 4).
 __global__ __launch_bounds__(kThreads) void k_pages_plan(const PagesParams p) {
-  __shared__ long long sh[kThreads / 64];
+  __shared__ int sh[kThreads / 64];
   if ((int)blockIdx.x < p.nc) {
-    int r[kPer], n = 0;
-    chunk_refs(p.refs, p.nb, blockIdx.x, 1, r);
-#pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-      const int page = blockIdx.x * kChunk + threadIdx.x * kPer + u;
-      n += r[u] <= 0;
-      if (p.refs_out != p.refs && page < p.nb) p.refs_out[page] = r[u];
-    }
-    const long long sum = block_sum(n, sh);
-    if (threadIdx.x == 0) p.counts[blockIdx.x] = (int)sum;
+    list_chunk<false>(p, blockIdx.x, sh);
     return;
   }
   const int lane = threadIdx.x & 63, i = (blockIdx.x - p.nc) * (kThreads / 64) + (threadIdx.x >> 6);
@@ -210,20 +259,27 @@ __global__ __launch_bounds__(kThreads) void k_pages_plan(const PagesParams p) {
   int bits = 0, len, n;
   const bool writes = appends(p, i, &len, &n, &bits);
   int tail = -1;
-  if (writes && len < (long long)p.mb * kBlock) {
+  if (writes) {
     const int page = last_page(p, i, len);
     if ((unsigned)page >= (unsigned)p.nb) {
       bits |= HOOK_PAGES_BAD_PAGE;
     } else {
+      constexpr int kRowsAhead = 4;
       int holders = p.refs[page];
-      for (int j0 = 0; holders > 1 && j0 < i; j0 += 64) {
-        const int j = j0 + lane;
-        bool leaves = false;
-        if (j < i) {
-          int len_j, n_j, ignored = 0;
-          leaves = appends(p, j, &len_j, &n_j, &ignored) && last_page(p, j, len_j) == page;
+      for (int j0 = 0; holders > 1 && j0 < i; j0 += 64 * kRowsAhead) {
+        int at[kRowsAhead];
+        bool partly[kRowsAhead];
+#pragma unroll
+        for (int u = 0; u < kRowsAhead; ++u) {
+          const int j = j0 + u * 64 + lane;
+          int n_j, ignored = 0;
+          partly[u] = j < i && appends(p, j, &at[u], &n_j, &ignored);
         }
-        holders -= __popcll(__ballot(leaves));
+#pragma unroll
+        for (int u = 0; u < kRowsAhead; ++u) {
+          const bool leaves = partly[u] && last_page(p, j0 + u * 64 + lane, at[u]) == page;
+          holders -= __popcll(__ballot(leaves));
+        }
       }
       if (holders > 1) tail = page;
     }
@@ -232,199 +288,126 @@ __global__ __launch_bounds__(kThreads) void k_pages_plan(const PagesParams p) {
     const bool fits = (long long)len + n <= (long long)p.mb * kBlock;
     RowPlan plan;
     plan.start = pages_of(len) - (tail >= 0);
-    plan.need = !fits ? kTooMany : n > 0 ? pages_of(len + n) - plan.start : 0;
     plan.tail = tail;
     plan.len = len;
+    plan.grow = n;
     p.plan[i] = plan;
+    p.need[i] = !fits ? kTooMany : n > 0 ? pages_of(len + n) - plan.start : 0;
     report(p, bits);
   }
 }
 
-// Workgroups below nc hand out the free pages of a chunk; in the others kRowChunk table entries of a row are carried over, and the first of
-// a row's also writes its length and takes a copied page's holder away.
-__global__ __launch_bounds__(kThreads) void k_pages_assign(const PagesParams p, int chunks) {
+constexpr int kInFlight = 4;      // 16-byte pieces of a thread in flight
+
+// A workgroup takes a row and every `groups`-th cache.  The first of a row's writes its table entries, its length and the counts of
+// its pages; all of them copy the token rows of the page that the row leaves.
+template <int N>
+__global__ __launch_bounds__(kThreads) void k_pages_append(const PagesParams p, int groups, const CacheList<N> list) {
+  __shared__ Ranks ranks;
   __shared__ long long sh[kThreads / 64];
   __shared__ int shi[kThreads / 64];
-  __shared__ int freed[kChunk];
-  __shared__ long long ends[kThreads];      // pages needed up to and with a row of the tile
-  const int tid = threadIdx.x, b = blockIdx.x;
-  long long need = 0, all;
-  for (int i = tid; i < p.S; i += kThreads) need += p.plan[i].need;
-  need = block_sum(need, sh);
-  const long long base = counts_before(p, b, sh, &all);
-  const bool fits = need <= all;
-  if (b < p.nc) {
-    if (!fits) {
-      if (b == 0 && tid == 0) report(p, HOOK_PAGES_FULL);
-      return;
-    }
-    if (base >= need) return;
-    int r[kPer], n = 0, count;
-    chunk_refs(p.refs, p.nb, b, 1, r);
-#pragma unroll
-    for (int u = 0; u < kPer; ++u) n += r[u] <= 0;
-    int at = block_scan(n, shi, &count);
-#pragma unroll
-    for (int u = 0; u < kPer; ++u)
-      if (r[u] <= 0) freed[at++] = b * kChunk + tid * kPer + u;
-    __syncthreads();
-    const long long end = base + count < need ? base + count : need;      // pages base .. end - 1 of those handed out lie here
-    long long carry = 0;
-    for (int i0 = 0; i0 < p.S && carry < end; i0 += kThreads) {
-      const int i = i0 + tid;
-      int tile;
-      const int mine = i < p.S ? p.plan[i].need : 0;
-      const int before = block_scan(mine, shi, &tile);      // (a tile needs no more than there are pages)
-      ends[tid] = carry + before + mine;
-      __syncthreads();
-      const long long lo = base > carry ? base : carry, hi = end < carry + tile ? end : carry + tile;
-      for (long long k = lo + tid; k < hi; k += kThreads) {
-        int a = 0, z = kThreads - 1;      // first row with ends > k
-        while (a < z) {
-          const int mid = (a + z) >> 1;
-          if (ends[mid] > k) z = mid; else a = mid + 1;
-        }
-        const RowPlan plan = p.plan[i0 + a];
-        const int e = plan.start + (int)(k - (ends[a] - plan.need)), page = freed[k - base];
-        p.table_out[(size_t)(i0 + a) * p.mb + e] = page;
-        p.refs_out[page] = 1;
-      }
-      carry += tile;
-      __syncthreads();
-    }
-    return;
-  }
-  const int row = (b - p.nc) / chunks, e0 = ((b - p.nc) % chunks) * kRowChunk;
+  const int tid = threadIdx.x, row = blockIdx.x / groups, group = blockIdx.x - row * groups;
   const RowPlan plan = p.plan[row];
-  if (p.table_out != p.table) {
-    const int held = pages_of(plan.len), copied = fits && plan.tail >= 0 ? plan.start : -1;
-#pragma unroll
-    for (int u = 0; u < kRowChunk / kThreads; ++u) {
-      const int e = e0 + u * kThreads + tid;
-      if (e < held && e != copied) p.table_out[(size_t)row * p.mb + e] = p.table[(size_t)row * p.mb + e];
+  if (group > 0 && plan.tail < 0) return;
+  long long before = 0, total = 0;      // pages needed by the rows before this one, and by all
+  for (int i = tid; i < p.S; i += kThreads) {
+    const int n = p.need[i];
+    total += n;
+    if (i < row) before += n;
+  }
+  load_ranks(p, ranks, shi);
+  total = block_sum(total, sh);
+  const bool fits = total <= ranks.before[kThreads];
+  if (group == 0) {
+    if (p.table_out != p.table) {
+      const int held = pages_of(plan.len), copied = fits && plan.tail >= 0 ? plan.start : -1;
+      for (int e = tid; e < held; e += kThreads)
+        if (e != copied) p.table_out[(size_t)row * p.mb + e] = p.table[(size_t)row * p.mb + e];
+    }
+    if (tid == 0) {
+      p.lens_out[row] = fits ? plan.len + plan.grow : plan.len;
+      if (!fits && row == 0) report(p, HOOK_PAGES_FULL);
+      if (fits && plan.tail >= 0) atomicSub(&p.refs_out[plan.tail], 1);
     }
   }
-  if (e0 == 0 && tid == 0) {
-    p.lens_out[row] = fits ? plan.len + max(p.cu[row + 1] - p.cu[row], 0) : plan.len;
-    if (plan.tail >= 0) {
-      if (fits) atomicSub(&p.refs_out[plan.tail], 1);
-      else p.plan[row].tail = -1;      // nothing is copied
+  if (!fits) return;
+  const int first = (int)block_sum(before, sh);
+  if (group == 0) {
+    const int need = p.need[row];
+    for (int k = tid; k < need; k += kThreads) {
+      const int page = page_by_number<false>(p, ranks, first + k);
+      p.table_out[(size_t)row * p.mb + plan.start + k] = page;
+      p.refs_out[page] = 1;
     }
   }
-}
-
-// The first token rows of the pages that rows leave: a workgroup takes one row and every `groups`-th cache.
-__global__ __launch_bounds__(kThreads) void k_pages_copy_tails(const PagesParams p, int groups) {
-  const int row = blockIdx.x / groups;
-  const RowPlan plan = p.plan[row];
   if (plan.tail < 0) return;
-  const int to = p.table_out[(size_t)row * p.mb + plan.start];
-  const int run = plan.len % kBlock * p.row_chunks, head = kBlock * p.row_chunks;      // 16-byte pieces copied and held of a head
+  const int to = page_by_number<false>(p, ranks, first);
+  const unsigned run = plan.len % kBlock * p.row_chunks, head = kBlock * p.row_chunks;      // 16-byte pieces copied and held of a head
   const size_t page = (size_t)p.heads * head;
-  for (int c = blockIdx.x % groups; c < p.ncaches; c += groups) {
-    uint4* const cache = static_cast<uint4*>(p.cache[c]);
+  const unsigned pieces = p.heads * run;
+  for (int c = group; c < p.ncaches; c += groups) {
+    uint4* const cache = static_cast<uint4*>(list.cache[c]);
     const uint4* const src = cache + (size_t)plan.tail * page;
     uint4* const dst = cache + (size_t)to * page;
-    for (int x = threadIdx.x; x < p.heads * run; x += kThreads) {
-      const int h = x / run, at = h * head + (x - h * run);
-      dst[at] = src[at];
+    for (unsigned x0 = tid; x0 < pieces; x0 += kInFlight * kThreads) {
+      uint4 v[kInFlight];
+      unsigned at[kInFlight];
+#pragma unroll
+      for (int u = 0; u < kInFlight; ++u) {
+        const unsigned x = x0 + u * kThreads, h = x / run;
+        at[u] = h * head + (x - h * run);
+        if (x < pieces) v[u] = src[at[u]];      // (a last page was written not long ago)
+      }
+#pragma unroll
+      for (int u = 0; u < kInFlight; ++u)
+        if (x0 + u * kThreads < pieces) store_stream16(&dst[at[u]], v[u]);
     }
   }
 }
 
 // ---- compact --------------------------------------------------------------------------------------------
 
-__global__ __launch_bounds__(kThreads) void k_pages_count_live(const PagesParams p) {
-  __shared__ long long sh[kThreads / 64];
-  int r[kPer], n = 0;
-  chunk_refs(p.refs, p.nb, blockIdx.x, 0, r);
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    const int page = blockIdx.x * kChunk + threadIdx.x * kPer + u;
-    n += r[u] > 0;
-    if (p.refs_out != p.refs && page < p.nb) p.refs_out[page] = r[u];
-  }
-  const long long sum = block_sum(n, sh);
-  if (threadIdx.x == 0) p.counts[blockIdx.x] = (int)sum;
+__global__ __launch_bounds__(kThreads) void k_pages_list(const PagesParams p) {
+  __shared__ int sh[kThreads / 64];
+  list_chunk<true>(p, blockIdx.x, sh);
 }
 
-// Ranks the pages that move and the holes that they move to.  order[page]: rank among the moving pages, -1 (a live page that
-// stays) or -2 (free).
-__global__ __launch_bounds__(kThreads) void k_pages_rank(const PagesParams p) {
-  __shared__ long long sh[kThreads / 64];
+constexpr int kPiece = kThreads * kInFlight;      // 16-byte pieces of a page that a workgroup moves at a time
+
+// Three kinds of workgroups: the data, the map and the counts, and the table rows.  With `live` live pages, `moves` of them at or above
+// number `live`, the moving pages are the last `moves` live ones and the holes the first `moves` free ones.
+template <int N>
+__global__ __launch_bounds__(kThreads) void k_pages_move(const PagesParams p, int movers, int mappers, int chunks, const CacheList<N> list) {
+  __shared__ Ranks ranks;
   __shared__ int shi[kThreads / 64];
-  const int tid = threadIdx.x, b = blockIdx.x;
-  long long all;
-  const long long base = counts_before(p, b, sh, &all);
-  const int live = (int)all;
-  // live pages below `live`: those of the chunks before the one that `live` lies in, and some of that one's
-  const int border = live / kChunk;
-  long long below = 0;
-  for (int c = tid; c < border && c < p.nc; c += kThreads) below += p.counts[c];
-  if (border < p.nc) {
-    int r[kPer];
-    chunk_refs(p.refs, p.nb, border, 0, r);
-#pragma unroll
-    for (int u = 0; u < kPer; ++u) below += r[u] > 0 && border * kChunk + tid * kPer + u < live;
-  }
-  below = block_sum(below, sh);
-  int r[kPer], n = 0, count;
-  chunk_refs(p.refs, p.nb, b, 0, r);
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) n += r[u] > 0;
-  int rank = (int)base + block_scan(n, shi, &count);      // live pages before this one
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    const int page = b * kChunk + tid * kPer + u;
-    if (page >= p.nb) break;
-    int order = -2;
-    if (r[u] > 0) {
-      order = -1;
-      if (page >= live) {
-        order = rank - (int)below;
-        p.movers[order] = page;
-      } else {
-        p.page_map[page] = page;
-      }
-      ++rank;
-    } else {
-      if (page < live) p.holes[page - rank] = page;
-      p.page_map[page] = -1;
-    }
-    p.order[page] = order;
-  }
-  if (b == 0 && tid == 0) {
-    *p.moves = live - (int)below;
-    *p.num_live = live;
-  }
-}
-
-constexpr int kMoveInFlight = 4;
-constexpr int kPiece = kThreads * kMoveInFlight;      // 16-byte pieces of a page that a workgroup moves at a time
-
-// Three kinds of workgroups: counts and map of the moved pages, table rows, and the data.
-__global__ __launch_bounds__(kThreads) void k_pages_move(const PagesParams p, int fixers, int chunks, int movers) {
   const int tid = threadIdx.x;
+  load_ranks(p, ranks, shi);
+  const int live = p.nb - ranks.before[kThreads];
+  int moves = 0;
+  if (live < p.nb) {
+    const int chunk = live / kChunk, order = p.order[live];
+    moves = frees_before(p, ranks, chunk) + (order < 0 ? -1 - order : live - chunk * kChunk - order);
+  }
+  const int stay = live - moves;
   int b = blockIdx.x;
   if (b < movers) {
-    const int moves = *p.moves;
     const int page = p.heads * kBlock * p.row_chunks, pieces = (page + kPiece - 1) / kPiece;
+    // (the pages of one cache are moved one after the other, so that workgroups that run together work on neighbours)
     const long long items = (long long)moves * p.ncaches * pieces;
     for (long long x = b; x < items; x += movers) {
-      const int piece = (int)(x % pieces);
       const long long rest = x / pieces;
-      const int c = (int)(rest % p.ncaches), k = (int)(rest / p.ncaches);
-      uint4* const cache = static_cast<uint4*>(p.cache[c]);
-      const uint4* const src = cache + (size_t)p.movers[k] * page;
-      uint4* const dst = cache + (size_t)p.holes[k] * page;
-      uint4 v[kMoveInFlight];
+      const int piece = (int)(x - rest * pieces), c = (int)(rest / moves), k = (int)(rest - (long long)c * moves);
+      uint4* const cache = static_cast<uint4*>(list.cache[c]);
+      const uint4* const src = cache + (size_t)page_by_number<true>(p, ranks, stay + k) * page;
+      uint4* const dst = cache + (size_t)page_by_number<false>(p, ranks, k) * page;
+      uint4 v[kInFlight];
 #pragma unroll
-      for (int u = 0; u < kMoveInFlight; ++u) {
+      for (int u = 0; u < kInFlight; ++u) {
         const int at = piece * kPiece + u * kThreads + tid;
-        if (at < page) v[u] = load_stream16(&src[at]);
+        if (at < page) v[u] = p.keep_lines ? src[at] : load_stream16(&src[at]);
       }
 #pragma unroll
-      for (int u = 0; u < kMoveInFlight; ++u) {
+      for (int u = 0; u < kInFlight; ++u) {
         const int at = piece * kPiece + u * kThreads + tid;
         if (at < page) store_stream16(&dst[at], v[u]);
       }
@@ -432,17 +415,27 @@ __global__ __launch_bounds__(kThreads) void k_pages_move(const PagesParams p, in
     return;
   }
   b -= movers;
-  if (b < fixers) {
-    const int k = b * kThreads + tid;
-    if (k < *p.moves) {
-      const int from = p.movers[k], to = p.holes[k];
-      p.page_map[from] = to;
-      p.refs_out[to] = p.refs[from];      // (a moving page's count is read and written by this thread alone)
-      p.refs_out[from] = 0;
+  // the page that takes over what page `page` holds, or -1 for a free one
+  auto moved = [&](int page) {
+    const int order = p.order[page];
+    if (order < 0) return -1;
+    if (page < live) return page;
+    const int chunk = page / kChunk, number = chunk * kChunk - frees_before(p, ranks, chunk) + order;
+    return page_by_number<false>(p, ranks, number - stay);
+  };
+  if (b < mappers) {
+    const int page = b * kThreads + tid;
+    if (b == 0 && tid == 0) *p.num_live = live;
+    if (page >= p.nb) return;
+    const int to = moved(page);
+    p.page_map[page] = to;
+    if (to >= 0 && to != page) {      // (counts of a moving page and of its hole are read and written by this thread alone)
+      p.refs_out[to] = p.refs[page];
+      p.refs_out[page] = 0;
     }
     return;
   }
-  b -= fixers;
+  b -= mappers;
   const int row = b / chunks, e0 = (b % chunks) * kRowChunk;
   int bits = 0;
   const int held = pages_of(length_of(p.lens[row], p.mb, &bits));
@@ -451,13 +444,9 @@ __global__ __launch_bounds__(kThreads) void k_pages_move(const PagesParams p, in
     const int e = e0 + u * kThreads + tid;
     if (e >= held) continue;
     int page = p.table[(size_t)row * p.mb + e];
-    if ((unsigned)page >= (unsigned)p.nb) {
-      bits |= HOOK_PAGES_BAD_PAGE;
-    } else {
-      const int order = p.order[page];
-      if (order >= 0) page = p.holes[order];
-      else if (order == -2) bits |= HOOK_PAGES_BAD_PAGE;
-    }
+    const int to = (unsigned)page < (unsigned)p.nb ? moved(page) : -1;
+    if (to < 0) bits |= HOOK_PAGES_BAD_PAGE;
+    else page = to;
     p.table_out[(size_t)row * p.mb + e] = page;
   }
   report(p, bits);
@@ -468,19 +457,19 @@ __global__ __launch_bounds__(kThreads) void k_pages_move(const PagesParams p, in
 inline size_t align16(size_t x) { return (x + 15) / 16 * 16; }
 
 struct Scratch {
-  size_t plan, counts, moves, order, movers, holes, bytes;
+  size_t plan, need, counts, free_list, live_list, order, bytes;
 };
 
 Scratch scratch_of(int S, int nb) {
   Scratch s;
   const size_t nc = ((size_t)nb + kChunk - 1) / kChunk;
   s.plan = 0;
-  s.moves = align16(sizeof(RowPlan) * (size_t)S);
-  s.counts = s.moves + 16;
-  s.order = s.counts + align16(4 * nc);
-  s.movers = s.order + align16(4 * (size_t)nb);
-  s.holes = s.movers + align16(4 * ((size_t)nb / 2 + 1));
-  s.bytes = s.holes + align16(4 * ((size_t)nb / 2 + 1));
+  s.need = align16(sizeof(RowPlan) * (size_t)S);
+  s.counts = s.need + align16(4 * (size_t)S);
+  s.free_list = s.counts + align16(4 * nc);
+  s.live_list = s.free_list + 4 * nc * kChunk;
+  s.order = s.live_list + 4 * nc * kChunk;
+  s.bytes = s.order + align16(4 * (size_t)nb);
   return s;
 }
 
@@ -521,7 +510,6 @@ hook_status prepare(const hook_pages_args* a, PagesParams* p) {
     for (int c = 0; c < a->num_caches; ++c) {
       if (!a->caches[c]) return HOOK_ERR_NULL;
       if (reinterpret_cast<uintptr_t>(a->caches[c]) % 16 != 0) return HOOK_ERR_UNSUPPORTED;
-      p->cache[c] = a->caches[c];
     }
     p->heads = a->num_kv_heads;
     p->row_chunks = (int)(a->row_bytes / 16);
@@ -532,12 +520,18 @@ hook_status prepare(const hook_pages_args* a, PagesParams* p) {
   char* ws = static_cast<char*>(a->workspace);
   p->nc = (a->num_blocks + kChunk - 1) / kChunk;
   p->plan = reinterpret_cast<RowPlan*>(ws + s.plan);
-  p->moves = reinterpret_cast<int*>(ws + s.moves);
+  p->need = reinterpret_cast<int*>(ws + s.need);
   p->counts = reinterpret_cast<int*>(ws + s.counts);
+  p->free_list = reinterpret_cast<int*>(ws + s.free_list);
+  p->live_list = reinterpret_cast<int*>(ws + s.live_list);
   p->order = reinterpret_cast<int*>(ws + s.order);
-  p->movers = reinterpret_cast<int*>(ws + s.movers);
-  p->holes = reinterpret_cast<int*>(ws + s.holes);
   return HOOK_OK;
+}
+
+template <int N> CacheList<N> list_of(const hook_pages_args* a) {
+  CacheList<N> list{};
+  for (int c = 0; c < a->num_caches; ++c) list.cache[c] = a->caches[c];
+  return list;
 }
 
 }  // namespace
@@ -591,18 +585,19 @@ hook_status hook_pages_append(const hook_pages_args* a) {
   PagesParams p = params_of(a);
   const hook_status checked = prepare(a, &p);
   if (checked != HOOK_OK) return checked;
-  const long long chunks = row_chunks_of(a);
   // a workgroup per row and cache while those are few, then caches take turns
-  int groups = p.ncaches;
-  while (groups > 1 && (long long)groups * p.S > 8192) groups = (groups + 1) / 2;
-  if (!grid_fits(p.nc + (long long)p.S * chunks) || !grid_fits((long long)p.S * (groups > 0 ? groups : 1))) return HOOK_ERR_UNSUPPORTED;
-  hipStream_t st = static_cast<hipStream_t>(a->stream);
+  int groups = p.ncaches > 0 ? p.ncaches : 1;
+  while (groups > 1 && (long long)groups * p.S > 4096) groups = (groups + 1) / 2;
   const int waves = kThreads / 64;
+  if (!grid_fits((long long)p.S * groups)) return HOOK_ERR_UNSUPPORTED;
+  if (p.S == 0 && p.refs == p.refs_out) return HOOK_OK;
+  hipStream_t st = static_cast<hipStream_t>(a->stream);
   hipLaunchKernelGGL(k_pages_plan, dim3((unsigned)(p.nc + (p.S + waves - 1) / waves)), dim3(kThreads), 0, st, p);
   if (hipGetLastError() != hipSuccess) return HOOK_ERR_LAUNCH;
-  hipLaunchKernelGGL(k_pages_assign, dim3((unsigned)(p.nc + p.S * chunks)), dim3(kThreads), 0, st, p, (int)chunks);
-  if (hipGetLastError() != hipSuccess) return HOOK_ERR_LAUNCH;
-  if (p.S > 0 && groups > 0) hipLaunchKernelGGL(k_pages_copy_tails, dim3((unsigned)(p.S * groups)), dim3(kThreads), 0, st, p, groups);
+  const dim3 grid((unsigned)(p.S * groups));
+  if (p.S == 0) return HOOK_OK;
+  if (p.ncaches <= kFewCaches) hipLaunchKernelGGL(k_pages_append<kFewCaches>, grid, dim3(kThreads), 0, st, p, groups, list_of<kFewCaches>(a));
+  else hipLaunchKernelGGL(k_pages_append<HOOK_PAGES_MAX_CACHES>, grid, dim3(kThreads), 0, st, p, groups, list_of<HOOK_PAGES_MAX_CACHES>(a));
   return hipGetLastError() == hipSuccess ? HOOK_OK : HOOK_ERR_LAUNCH;
 }
 
@@ -620,14 +615,19 @@ hook_status hook_pages_compact(const hook_pages_args* a) {
   const hook_status checked = prepare(a, &p);
   if (checked != HOOK_OK) return checked;
   const long long chunks = row_chunks_of(a);
-  const int fixers = (p.nb / 2 + kThreads) / kThreads, movers = p.ncaches > 0 ? 2048 : 0;
-  if (!grid_fits(movers + fixers + p.S * chunks)) return HOOK_ERR_UNSUPPORTED;
+  const int mappers = (p.nb + kThreads - 1) / kThreads, movers = p.ncaches > 0 ? 1024 : 0;
+  // Ordinary loads where all caches together fit 256 MB of last-level cache, streaming ones otherwise: 8 caches of 512 pages of 32 KB 16.7 and
+  // 18.2 us, of 8192 pages 218 and 205.
+  p.keep_lines = (long long)p.ncaches * p.nb * p.heads * kBlock * p.row_chunks * 16 <= (256ll << 20);
+  if (!grid_fits(movers + mappers + p.S * chunks)) return HOOK_ERR_UNSUPPORTED;
   hipStream_t st = static_cast<hipStream_t>(a->stream);
-  hipLaunchKernelGGL(k_pages_count_live, dim3((unsigned)p.nc), dim3(kThreads), 0, st, p);
+  hipLaunchKernelGGL(k_pages_list, dim3((unsigned)p.nc), dim3(kThreads), 0, st, p);
   if (hipGetLastError() != hipSuccess) return HOOK_ERR_LAUNCH;
-  hipLaunchKernelGGL(k_pages_rank, dim3((unsigned)p.nc), dim3(kThreads), 0, st, p);
-  if (hipGetLastError() != hipSuccess) return HOOK_ERR_LAUNCH;
-  hipLaunchKernelGGL(k_pages_move, dim3((unsigned)(movers + fixers + p.S * chunks)), dim3(kThreads), 0, st, p, fixers, (int)chunks, movers);
+  const dim3 grid((unsigned)(movers + mappers + p.S * chunks));
+  if (p.ncaches <= kFewCaches)
+    hipLaunchKernelGGL(k_pages_move<kFewCaches>, grid, dim3(kThreads), 0, st, p, movers, mappers, (int)chunks, list_of<kFewCaches>(a));
+  else
+    hipLaunchKernelGGL(k_pages_move<HOOK_PAGES_MAX_CACHES>, grid, dim3(kThreads), 0, st, p, movers, mappers, (int)chunks, list_of<HOOK_PAGES_MAX_CACHES>(a));
   return hipGetLastError() == hipSuccess ? HOOK_OK : HOOK_ERR_LAUNCH;
 }
 
