@@ -69,7 +69,7 @@ def check_table(got, rows, before=None):
         assert got[i][len(row):] == rest, i
 
 
-STATES = [(1, 1, 16, 3), (1, 4, 60, 9), (3, 8, 100, 20), (9, 40, 500, 60), (64, 30, 400, 200), (65, 1100, 17000, 50), (300, 20, 300, 900), (7, 2100, 30000, 2500)]
+STATES = [(1, 1, 16, 3), (1, 4, 60, 9), (3, 8, 100, 20), (9, 40, 500, 60), (64, 30, 400, 200), (65, 1100, 17000, 50), (300, 20, 300, 900), (7, 2100, 30000, 2500), (900, 12, 150, 400), (3, 4500, 71000, 10)]
 
 
 @pytest.mark.parametrize("S,mb,most,spare", STATES)
