@@ -497,7 +497,7 @@ hook_status hook_reduce_mass(const hook_reduce_args* args);
  * the rows go to the slots of the batch's new tokens (num_tokens = cu_q_lens[num_seqs]), bit for bit as by the two calls,
  * quantised for an 8-bit cache; tokens are dropped by the same rules.  k_out may then be null (the keys go to the cache alone).
  * Any head_dim up to HOOK_ROPE_MAX_DIM and any even rotary_dim; rows, halves and pointers that are multiples of 16 bytes run at
- * full speed, others at that of the largest power of two that divides them.  Pointers are aligned to their elements.
+ * full speed, others with loads of the largest power of two that divides them (of single elements: half of it).  Pointers are aligned to their elements.
  */
 #define HOOK_ROPE_MAX_AXES 4
 #define HOOK_ROPE_MAX_DIM 512

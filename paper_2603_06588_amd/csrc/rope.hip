@@ -2,10 +2,11 @@
 // into its pages.  Per pair (x1, x2) of a head and its angle a:  (x1 cos a - x2 sin a, x2 cos a + x1 sin a).
 //
 // Bound by memory: every element is read once and written once (keys twice where both outputs are asked for).  The angles
-// of a token are the same in all its heads, so a workgroup takes one or more whole tokens, lets a wave compute each token's
-// cosines and sines once into shared memory (a lane per pair) while another finds the token's slot in the cache, and
-// then walks the token's heads by units of 2 W elements - the two halves of W pairs, or W neighbouring pairs - of which
-// W is what one load can carry.  The first unit is requested before the angles are computed.
+// of a token are the same in all its heads, so a workgroup takes a token, lets one wave compute its cosines and sines
+// once into shared memory (a lane per pair) while another finds the token's slot in the cache, and then walks the token's heads by units of two vectors of what one load carries: the two halves of as many pairs, or neighbouring
+// pairs in each.  The first units are requested before the angles are computed.
+// 16384 tokens of 64 query and 8 key and value heads of 128 into the cache: 120 us, 5.9 TB/s (two tokens to a workgroup 123, four 137;
+// threads 128 / 512: 127 / 139); 8000 tokens of 32 and 8: 40 us, neighbouring pairs 39, 8-bit cache 43.
 #include "../../include/hook_api.h"
 #include "kv_write_device.h"
 
@@ -13,8 +14,7 @@ namespace hook {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeMaxTokens = 4;     // tokens of a workgroup
-constexpr int kRopeInFlight = 2;      // units that a thread requests together
+constexpr int kRopeInFlight = 2;      // units that a thread requests together (one and three: 123 and 122 us)
 
 struct RopeParams {
   int T, Hq, Hk, Hv, d, pairs;        // Hk, Hv: 0 where k is not rotated, or no cache is written
@@ -90,36 +90,36 @@ __device__ __forceinline__ int find_sequence(const int* cu, int n, int row, int 
   return lo;
 }
 
-template <typename E, int W, bool NEIGHBOURS, int TT>
+template <typename E, int W, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int parts) {
-  __shared__ float sh_cos[TT][HOOK_ROPE_MAX_DIM / 2], sh_sin[TT][HOOK_ROPE_MAX_DIM / 2];
-  __shared__ long long sh_row[TT];    // blk * Hkv * 16 + slot of the token in the cache, or -1
+  __shared__ float sh_cos[HOOK_ROPE_MAX_DIM / 2], sh_sin[HOOK_ROPE_MAX_DIM / 2];
+  __shared__ long long sh_row;        // blk * Hkv * 16 + slot of the token in the cache, or -1
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int part = blockIdx.x % parts, t0 = (blockIdx.x / parts) * TT;
-  const int tokens = min(TT, p.T - t0);
+  const int t = blockIdx.x / parts, part = blockIdx.x - t * parts;
   const int units = (p.d + 2 * W - 1) / (2 * W);                // of a head: the turned ones, then the rest of it
-  const int per_token = (p.Hq + p.Hk + p.Hv) * units, total = tokens * per_token;
+  const int total = (p.Hq + p.Hk + p.Hv) * units;
   const int turned = p.pairs / W;
 
   Vec<E, W> x[kRopeInFlight][2];
-  // where unit e of the workgroup lies: token, head (queries, keys, values in a row) and the elements of its two vectors
-  struct Unit { int t, h, a, b; };                              // b < 0: the head ends inside the unit
+  // where unit e of the token lies: head (queries, keys, values in a row) and the elements of its two vectors
+  struct Unit { int h, a, b; };                                 // b < 0: the head ends inside the unit
   auto unit = [&](int e) {
     Unit u;
-    u.t = TT == 1 ? 0 : e / per_token;
-    const int in = e - u.t * per_token;
-    u.h = in / units;
-    const int c = in - u.h * units;
-    const bool turns = u.h < p.Hq + p.Hk && c < turned;
-    if (turns && !NEIGHBOURS) {
+    u.h = e / units;
+    const int c = e - u.h * units;
+    // the unit's vectors lie apart rather than side by side, so that neighbouring lanes load neighbouring vectors
+    if (NEIGHBOURS && W == 1 && u.h < p.Hq + p.Hk) {
+      u.a = 2 * c;
+      u.b = u.a + 1;
+    } else if (NEIGHBOURS || u.h >= p.Hq + p.Hk) {
+      u.a = c * W;
+      u.b = (units + c) * W;
+    } else if (c < turned) {
       u.a = c * W;
       u.b = p.pairs + c * W;
-    } else if (u.h >= p.Hq + p.Hk || NEIGHBOURS) {
-      u.a = 2 * c * W;
-      u.b = u.a + W;
     } else {                                                    // behind both halves
-      u.a = 2 * c * W;
-      u.b = u.a + W;
+      u.a = (turned + c) * W;
+      u.b = (units + c) * W;
     }
     if (u.b + W > p.d) u.b = -1;
     return u;
@@ -131,9 +131,9 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int p
       if (e >= total) break;
       const Unit u = unit(e);
       const char* src;
-      if (u.h < p.Hq) src = p.q + (t0 + u.t) * p.q_stride + (size_t)u.h * p.d * sizeof(E);
-      else if (u.h < p.Hq + p.Hk) src = p.k + (t0 + u.t) * p.k_stride + (size_t)(u.h - p.Hq) * p.d * sizeof(E);
-      else src = p.v + (t0 + u.t) * p.v_stride + (size_t)(u.h - p.Hq - p.Hk) * p.d * sizeof(E);
+      if (u.h < p.Hq) src = p.q + t * p.q_stride + (size_t)u.h * p.d * sizeof(E);
+      else if (u.h < p.Hq + p.Hk) src = p.k + t * p.k_stride + (size_t)(u.h - p.Hq) * p.d * sizeof(E);
+      else src = p.v + t * p.v_stride + (size_t)(u.h - p.Hq - p.Hk) * p.d * sizeof(E);
       x[i][0] = load_vec<E, W>(src + (size_t)u.a * sizeof(E));
       if (u.b >= 0) x[i][1] = load_vec<E, W>(src + (size_t)u.b * sizeof(E));
     }
@@ -141,44 +141,39 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int p
   const int first = part * kRopeThreads + tid;
   request(first);
 
-  // one wave per token for its angles, another for its slot
-  for (int job = wave; job < 2 * TT; job += kRopeThreads / 64) {
-    const int t = job >> 1;
-    if (t >= tokens) continue;
-    if ((job & 1) == 0) {
-      for (int c = lane; c < p.pairs; c += 64) {
-        int axis = 0;
-        if (p.cyclic) {
-          const int a = c % p.axes;
-          axis = c / p.axes < p.axis_pairs[a] ? a : 0;
-        } else {
-          for (int a = 0, end = 0; a + 1 < p.axes; ++a) {
-            end += p.axis_pairs[a];
-            if (c >= end) axis = a + 1;
-          }
+  if (wave == 0) {
+    for (int c = lane; c < p.pairs; c += 64) {
+      int axis = 0;
+      if (p.cyclic) {
+        const int a = c % p.axes;
+        axis = c / p.axes < p.axis_pairs[a] ? a : 0;
+      } else {
+        for (int a = 0, end = 0; a + 1 < p.axes; ++a) {
+          end += p.axis_pairs[a];
+          if (c >= end) axis = a + 1;
         }
-        // the angle in half turns, reduced to [-1, 1] in fp64: positions of a million still leave 30 bits of it
-        double turns = (double)p.positions[(size_t)axis * p.T + t0 + t] * ((double)p.inv_freq[c] * 0.15915494309189533577);
-        turns -= __builtin_rint(turns);
-        float sn, cs;
-        sincospif(2.0f * (float)turns, &sn, &cs);
-        sh_cos[t][c] = cs * p.magnitude;
-        sh_sin[t][c] = sn * p.sign;
       }
-    } else if (p.Hv > 0) {
-      const int row = t0 + t, i = find_sequence(p.cu, p.num_seqs, row, lane);
-      if (lane == 0) {
-        const int begin = p.cu[i], n = p.cu[i + 1] - begin, L = p.seq_lens[i], at = row - begin;
-        long long r = -1;
-        if (begin >= 0 && at >= 0 && at < n && n <= L) {
-          const int pos = L - n + at;
-          if ((pos >> 4) < p.max_blocks) {
-            const int blk = p.block_table[(size_t)i * p.max_blocks + (pos >> 4)];
-            if ((unsigned)blk < (unsigned)p.num_blocks) r = (long long)blk * p.Hv * kBlock + (pos & 15);
-          }
+      // the angle in half turns, reduced to [-1, 1] in fp64: positions of a million still leave 30 bits of it
+      double turns = (double)p.positions[(size_t)axis * p.T + t] * ((double)p.inv_freq[c] * 0.15915494309189533577);
+      turns -= __builtin_rint(turns);
+      float sn, cs;
+      sincospif(2.0f * (float)turns, &sn, &cs);
+      sh_cos[c] = cs * p.magnitude;
+      sh_sin[c] = sn * p.sign;
+    }
+  } else if (wave == 1 && p.Hv > 0) {
+    const int i = find_sequence(p.cu, p.num_seqs, t, lane);
+    if (lane == 0) {
+      const int begin = p.cu[i], n = p.cu[i + 1] - begin, L = p.seq_lens[i], at = t - begin;
+      long long r = -1;
+      if (begin >= 0 && at >= 0 && at < n && n <= L) {
+        const int pos = L - n + at;
+        if ((pos >> 4) < p.max_blocks) {
+          const int blk = p.block_table[(size_t)i * p.max_blocks + (pos >> 4)];
+          if ((unsigned)blk < (unsigned)p.num_blocks) r = (long long)blk * p.Hv * kBlock + (pos & 15);
         }
-        sh_row[t] = r;
       }
+      sh_row = r;
     }
   }
   __syncthreads();
@@ -191,27 +186,35 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int p
       if (e >= total) break;
       const Unit u = unit(e);
       const bool value = u.h >= p.Hq + p.Hk, key = !value && u.h >= p.Hq;
-      const int c = (NEIGHBOURS ? u.a / 2 : u.a);              // first pair of the unit
-      if (!value && (NEIGHBOURS ? u.a < 2 * p.pairs : u.a < p.pairs)) {
+      auto turn = [&](E& lo, E& hi, int c) {
+        const float a = (float)lo, b = (float)hi, cs = sh_cos[c], sn = sh_sin[c];
+        lo = (E)(a * cs - b * sn);
+        hi = (E)(b * cs + a * sn);
+      };
+      if (!value) {
+        if constexpr (NEIGHBOURS && W > 1) {
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-          E& lo = NEIGHBOURS ? x[i][2 * j / W].e[2 * j % W] : x[i][0].e[j];
-          E& hi = NEIGHBOURS ? x[i][(2 * j + 1) / W].e[(2 * j + 1) % W] : x[i][1].e[j];
-          const float a = (float)lo, b = (float)hi, cs = sh_cos[u.t][c + j], sn = sh_sin[u.t][c + j];
-          lo = (E)(a * cs - b * sn);
-          hi = (E)(b * cs + a * sn);
+          for (int half = 0; half < 2; ++half) {
+            const int at = half == 0 ? u.a : u.b;
+            if (at < 0 || at >= 2 * p.pairs) continue;
+#pragma unroll
+            for (int j = 0; j < W; j += 2) turn(x[i][half].e[j], x[i][half].e[j + 1], (at + j) / 2);
+          }
+        } else if (NEIGHBOURS ? u.a < 2 * p.pairs : u.a < p.pairs) {
+#pragma unroll
+          for (int j = 0; j < W; ++j) turn(x[i][0].e[j], x[i][1].e[j], NEIGHBOURS ? u.a / 2 : u.a + j);
         }
       }
       char* dst = nullptr;
-      if (!value && !key) dst = p.q_out + (t0 + u.t) * p.q_out_stride + (size_t)u.h * p.d * sizeof(E);
-      else if (key && p.k_out) dst = p.k_out + (t0 + u.t) * p.k_out_stride + (size_t)(u.h - p.Hq) * p.d * sizeof(E);
+      if (!value && !key) dst = p.q_out + t * p.q_out_stride + (size_t)u.h * p.d * sizeof(E);
+      else if (key && p.k_out) dst = p.k_out + t * p.k_out_stride + (size_t)(u.h - p.Hq) * p.d * sizeof(E);
       if (dst) {
         store_vec<E, W>(dst + (size_t)u.a * sizeof(E), x[i][0]);
         if (u.b >= 0) store_vec<E, W>(dst + (size_t)u.b * sizeof(E), x[i][1]);
       }
-      if (p.Hv > 0 && (value || key) && sh_row[u.t] >= 0) {
+      if (p.Hv > 0 && (value || key) && sh_row >= 0) {
         const int g = value ? u.h - p.Hq - p.Hk : u.h - p.Hq;
-        const size_t row = (size_t)(sh_row[u.t] + (long long)g * kBlock) * p.d;
+        const size_t row = (size_t)(sh_row + (long long)g * kBlock) * p.d;
         char* cache = value ? p.v_cache : p.k_cache;
         if (p.kv8) {
           const float scale = value ? p.v_scale[g] : p.k_scale[g];
@@ -230,14 +233,10 @@ template <typename E, int W, bool NEIGHBOURS>
 hipError_t launch_width(const RopeParams& p, hipStream_t st) {
   const int units = (p.d + 2 * W - 1) / (2 * W);
   const long long per_token = (long long)(p.Hq + p.Hk + p.Hv) * units;
-  // Few tokens: a token's heads are cut over several workgroups, one round of units each, to be spread over the chip.  Many:
-  // four tokens to a workgroup, whose four waves compute an angle table each.
-  if (p.T >= 4096) {
-    hipLaunchKernelGGL((k_rope<E, W, NEIGHBOURS, kRopeMaxTokens>), dim3((unsigned)((p.T + kRopeMaxTokens - 1) / kRopeMaxTokens)), dim3(kRopeThreads), 0, st, p, 1);
-  } else {
-    const int parts = (int)((per_token + kRopeThreads - 1) / kRopeThreads);
-    hipLaunchKernelGGL((k_rope<E, W, NEIGHBOURS, 1>), dim3((unsigned)(p.T * parts)), dim3(kRopeThreads), 0, st, p, parts);
-  }
+  // Few tokens: a token's heads are cut over several workgroups, one round of units each, to be spread over the chip (2000 tokens of 32 and
+  // 8 heads 14.8 us so, 12.0 with a workgroup each; 1000 tokens 8.5 with either, where the launch counts).
+  const int parts = p.T >= 600 ? 1 : (int)((per_token + kRopeThreads - 1) / kRopeThreads);
+  hipLaunchKernelGGL((k_rope<E, W, NEIGHBOURS>), dim3((unsigned)(p.T * parts)), dim3(kRopeThreads), 0, st, p, parts);
   return hipGetLastError();
 }
 
