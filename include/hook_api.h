@@ -1,7 +1,8 @@
 /*
  * hook_api.h - C ABI of the hooked paged-attention library for MI355X (gfx950).
  *
- * Two operations, both asynchronous on a caller-supplied HIP stream:
+ * Two operations, both asynchronous on a caller-supplied HIP stream (and around them what a step of generation does with the same
+ * cache and the same rows: rotary positions, pages shared between sequences, adjusted logits, further below):
  *
  *   hook_attn_probe  causal grouped-query attention forward over a paged KV
  *                    cache which, for configured heads, also returns the softmax
@@ -26,7 +27,7 @@
  *     state between calls and never synchronises the stream.  The host reads only
  *     the scalar fields, so a call is a fixed sequence of kernel launches.
  *   - Inputs are read-only.  The only writes are `out`, `mass`, `workspace`
- *     (hook_attn_probe) and `hidden` (hook_steer).
+ *     (hook_attn_probe), `hidden` (hook_steer) and what the other calls name as their outputs.
  *   - Errors are returned as hook_status; nothing is launched or written when a
  *     call is rejected.  Contents of device arrays (block ids, lengths) cannot be
  *     checked without a sync: block ids outside [0, num_blocks) are clamped so a

@@ -470,6 +470,6 @@ const char* hook_status_string(hook_status s) {
   return "unknown status";
 }
 
-int hook_version(void) { return 2; }
+int hook_version(void) { return 3; }
 
 }  // extern "C"

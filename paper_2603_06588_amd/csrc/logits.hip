@@ -109,7 +109,7 @@ __device__ __forceinline__ void adjust(const LogitsParams& p, const Row& r, Shar
     __syncthreads();
     if (mine) {
       bool later = false;
-#pragma unroll 8
+#pragma unroll 4
       for (int i = 0; i < sh.num_biased; ++i) later |= sh.biased[i].y == (int)at & sh.biased[i].x > j;
       if (!later) {
         replace(at, true, p.bias_values[j]);
