@@ -240,6 +240,7 @@ extern "C" hook_status hook_steer_logits(const hook_steer_logits_args* a) {
   if (a->vocab > (1 << 30) || !grid_fits(((long long)a->num_rows + 8) * (a->vocab / 8192 + 2))) return HOOK_ERR_UNSUPPORTED;
   if (a->num_rows == 0 || a->vocab == 0) return HOOK_OK;
   const long long stride = a->logits_stride ? a->logits_stride : a->vocab, out_stride = a->out_stride ? a->out_stride : a->vocab;
+  if (stride > (1ll << 40) || out_stride > (1ll << 40)) return HOOK_ERR_UNSUPPORTED;
   if (stride < a->vocab || out_stride < a->vocab || (a->out == a->logits && stride != out_stride)) return HOOK_ERR_SHAPE;
   if (!a->logits || !a->out) return HOOK_ERR_NULL;
   if (a->history_len > 0 && (!a->history || !a->cu_history)) return HOOK_ERR_NULL;

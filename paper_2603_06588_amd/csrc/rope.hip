@@ -279,6 +279,8 @@ extern "C" hook_status hook_rope(const hook_rope_args* a) {
   auto stride = [](int64_t given, long long width) { return given ? (long long)given : width; };
   const long long qs = stride(a->q_stride, qw), ks = stride(a->k_stride, kw), vs = stride(a->v_stride, kw);
   const long long qos = stride(a->q_out_stride, qw), kos = stride(a->k_out_stride, kw);
+  for (long long x : {qs, ks, vs, qos, kos})
+    if (x > (1ll << 40)) return HOOK_ERR_UNSUPPORTED;
   if ((has_q && (qs < qw || qos < qw)) || (has_k && (ks < kw || kos < kw)) || (cache && vs < kw)) return HOOK_ERR_SHAPE;
   if ((has_q && a->q_out == a->q && qs != qos) || (has_k && a->k_out == a->k && ks != kos)) return HOOK_ERR_SHAPE;
   bool kv8 = false;

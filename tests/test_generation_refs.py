@@ -166,6 +166,7 @@ def test_rope_refusals(binding):
     assert _rope(binding, num_axes=2, axis_pairs=(31, 33), axis_order=1) == 2      # the second axis runs out of pairs
     assert _rope(binding, q_out=P, k_out=P, q_stride=100) == 2                     # rows on top of each other
     assert _rope(binding, q_out=P, k_out=2 * P, q_stride=1024, q_out_stride=2048) == 2      # its own input at another stride
+    assert _rope(binding, q_out=2 * P, k_out=P, q_stride=1 << 41) == 3
     assert _rope(binding, q=P + 1, q_out=P, k_out=P) == 3                          # not aligned to an element
     cache = dict(q_out=P, k_cache=P, v_cache=P, v=P, num_seqs=1, block_size=16, max_blocks_per_seq=4, num_blocks=4, block_table=P, seq_lens=P,
                  cu_q_lens=P)
@@ -245,6 +246,7 @@ def test_logits_refusals(binding):
     assert _logits(binding, vocab=1 << 29, num_rows=1 << 20) == 3
     assert _logits(binding, logits_stride=99) == 2 and _logits(binding, out_stride=99) == 2
     assert _logits(binding, logits_stride=104) == 2                               # its own input at another stride
+    assert _logits(binding, logits_stride=1 << 41, out=2 * P) == 3
     assert _logits(binding, logits=0) == 1 and _logits(binding, out=0) == 1
     assert _logits(binding, history_len=5, history=P) == 1 and _logits(binding, history_len=5, cu_history=P) == 1
     assert _logits(binding, bias_len=5, cu_bias=P, bias_ids=P) == 1

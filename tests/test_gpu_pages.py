@@ -333,6 +333,80 @@ def test_captured_graph_of_a_step():
         assert all(torch.equal(a, b) for a, b in zip(kept, eager))
 
 
+@pytest.mark.parametrize("which", [(0,), (1,), (2,), (0, 1), (1, 2), (0, 2)])
+def test_append_with_some_outputs_in_place(which):
+    """Table, lengths and counts may each be in place or not."""
+    p = Pool(21, 20, 12, 120, 40, share=0.8)
+    cu, status = list(range(21)), ints([0])
+    caches = new_caches(p.nb, 1, 16, torch.bfloat16, 2)
+    before = caches.clone()
+    ins = [ints(p.table()), ints(p.lens), ints(p.refs)]
+    outs = [t if i in which else torch.full_like(t, JUNK) for i, t in enumerate(ins)]
+    binding.hook_pages_append(ints(cu), *ins, caches, status, block_table_out=outs[0], seq_lens_out=outs[1], ref_counts_out=outs[2])
+    rows, L, counts, copies, bits = G.append(cu, p.table(), p.lens, p.refs)
+    check_table(outs[0], rows)
+    assert outs[1].tolist() == L and outs[2].tolist() == counts and int(status) == bits == 0 and len(copies) > 3
+    for a, b, n in copies:
+        before[:, b, :, :n] = before[:, a, :, :n]
+    assert torch.equal(caches, before)
+
+
+def test_many_caches_and_another_stream():
+    """More caches than the short argument list holds, on a stream that is not the current one, with the call's own scratch."""
+    p = Pool(31, 30, 12, 150, 60, share=0.8)
+    caches = list(new_caches(p.nb, 1, 16, torch.bfloat16, 40))
+    cu, status = ints(list(range(31))), ints([0])
+    t, L, c, page_map, live = ints(p.table()), ints(p.lens), ints(p.refs), ints([0] * p.nb), ints([0])
+    want = [x.clone() for x in caches]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    binding.hook_pages_append(cu, t, L, c, caches, status, stream=side)
+    binding.hook_pages_compact(t, L, c, caches, page_map, live, status, stream=side)
+    side.synchronize()
+    rows, lens, counts, copies, bits = G.append(list(range(31)), p.table(), p.lens, p.refs)
+    table = [r + [JUNK] * (12 - len(r)) for r in rows]
+    rows, counts, want_map, n, moves, _ = G.compact(table, lens, counts)
+    check_table(t, rows)
+    assert L.tolist() == lens and c.tolist() == counts and page_map.tolist() == want_map and int(live) == n and int(status) == 0
+    for x in want:
+        for a, b, k in copies:
+            x[b, :, :k] = x[a, :, :k]
+        for a, b in moves:
+            x[b] = x[a]
+    assert all(torch.equal(x, y) for x, y in zip(caches, want))
+
+
+def test_more_pages_than_segments():
+    """Over 256 chunks of 2048 pages: several chunks to a segment, free and live pages far apart."""
+    nb = 2048 * 600 + 77
+    g = torch.Generator().manual_seed(1)
+    refs = torch.ones(nb, dtype=torch.int32)
+    free = torch.randperm(nb, generator=g)[:5000]
+    refs[free] = 0
+    refs[2048 * 100:2048 * 300] = 0            # whole chunks without a live page
+    table, lens = [[nb - 1] + [0] * 400, [2048 * 350 + 5] + [0] * 400], [16, 5]
+    refs[nb - 1], refs[2048 * 350 + 5] = 1, 2
+    t, L, c, status = ints(table), ints(lens), refs.to(DEV), ints([0])
+    binding.hook_pages_append(ints([0, 6000, 6001]), t, L, c, [], status)
+    order = (refs == 0).nonzero()[:, 0].tolist()
+    want = [[nb - 1] + order[:375], [order[375]]]
+    check_table(t, want, table)
+    refs[order[:376]] = 1
+    refs[2048 * 350 + 5] = 1
+    assert L.tolist() == [6016, 6] and torch.equal(c.cpu(), refs) and int(status) == 0
+    page_map, live = torch.empty(nb, dtype=torch.int32, device=DEV), ints([0])
+    binding.hook_pages_compact(t, L, c, [], page_map, live, status)
+    alive = refs > 0
+    n = int(alive.sum())
+    at = torch.arange(nb)
+    movers, holes = at[alive & (at >= n)], at[~alive & (at < n)]
+    want_map = torch.where(alive, at, -1)
+    want_map[movers] = holes
+    assert int(live) == n and torch.equal(page_map.cpu().long(), want_map) and int(status) == 0
+    check_table(t, [[int(want_map[p]) for p in row] for row in want], table)
+    assert torch.equal(c.cpu() > 0, at < n)
+
+
 def test_refusals_of_the_binding():
     i, t = ints([0]), ints([[0, 0]])
     c = torch.zeros((1, 1, 16, 8), dtype=torch.bfloat16, device=DEV)
