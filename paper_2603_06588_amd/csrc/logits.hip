@@ -147,19 +147,6 @@ __global__ __launch_bounds__(NT) void k_steer_logits(const LogitsParams p, int r
   const E* const in = reinterpret_cast<const E*>(p.logits + row * p.stride);
   E* const out = reinterpret_cast<E*>(p.out + row * p.out_stride);
   const int skew = (int)(reinterpret_cast<uintptr_t>(in) / sizeof(E) % W), token0 = r0 - skew;
-  Raw raw[VPT];
-#pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int e = token0 + (i * NT + tid) * W;
-    if (e >= 0 && e + W <= p.V) {
-      raw[i] = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(in + e));
-    } else {      // the row's first or last tokens, fewer than a load
-      Vec<E, W> v;
-#pragma unroll
-      for (int u = 0; u < W; ++u) v.e[u] = e + u >= 0 && e + u < p.V ? in[e + u] : (E)0.0f;
-      __builtin_memcpy(&raw[i], &v, sizeof v);
-    }
-  }
   const int m = p.mask ? (p.mask_rows ? p.mask_rows[row] : row) : -1;
   const bool masked = m >= 0 && m < p.masks;
   const unsigned* const mask = p.mask + (masked ? (size_t)m * p.words : 0);
@@ -173,6 +160,23 @@ __global__ __launch_bounds__(NT) void k_steer_logits(const LogitsParams p, int r
       if ((e & 31) + W > 32 && e + W > 0 && word + 1 < p.words) hi = mask[word + 1];
       allowed[i] = (unsigned)((((unsigned long long)hi << 32) | lo) >> (e & 31));
     }
+  Raw raw[VPT];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int e = token0 + (i * NT + tid) * W;
+    // A load whose tokens are all barred is left out: 256 x 131072 bf16 with 2000 tokens of history each take 25.5 us where a grammar allows one
+    // token in 2000 (29.2 with all loads), 28.4 and 28.9 where it allows a quarter or all.
+    raw[i] = Raw{};
+    if (masked && (allowed[i] & ((1u << W) - 1u)) == 0) continue;
+    if (e >= 0 && e + W <= p.V) {
+      raw[i] = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(in + e));
+    } else {      // the row's first or last tokens, fewer than a load
+      Vec<E, W> v;
+#pragma unroll
+      for (int u = 0; u < W; ++u) v.e[u] = e + u >= 0 && e + u < p.V ? in[e + u] : (E)0.0f;
+      __builtin_memcpy(&raw[i], &v, sizeof v);
+    }
+  }
   Row r{};
   r.rep = p.repetition ? p.repetition[row] : 1.0f;
   r.freq = p.frequency ? p.frequency[row] : 0.0f;
