@@ -426,8 +426,6 @@ __global__ __launch_bounds__(kThreads) void k_pages_list(const PagesParams p) {
   list_chunk<true>(p, blockIdx.x, sh);
 }
 
-constexpr int kPiece = kThreads * kInFlight;      // 16-byte pieces of a page that a workgroup moves at a time
-
 // Three kinds of workgroups: the data, the map and the counts, and the table rows.  With `live` live pages, `moves` of them at or above
 // number `live`, the moving pages are the last `moves` live ones and the holes the first `moves` free ones.
 template <int N>
@@ -445,10 +443,13 @@ __global__ __launch_bounds__(kThreads) void k_pages_move(const PagesParams p, in
   const int stay = live - moves;
   int b = blockIdx.x;
   if (b < movers) {
-    const int page = p.heads * kBlock * p.row_chunks, pieces = (page + kPiece - 1) / kPiece;
+    // A piece of a page to the workgroup, or one to each of its waves where a page is less than the workgroup moves at a time (7000 pages
+    // of 4 KB in 8 caches: 45 and 26 us; 8192 of 32 KB 202 and 205)
+    const int page = p.heads * kBlock * p.row_chunks, threads = page >= kThreads * kInFlight ? kThreads : 64, lane = tid & (threads - 1);
+    const int size = threads * kInFlight, pieces = (page + size - 1) / size, each = kThreads / threads;
     // (the pages of one cache are moved one after the other, so that workgroups that run together work on neighbours)
     const long long items = (long long)moves * p.ncaches * pieces;
-    for (long long x = b; x < items; x += movers) {
+    for (long long x = (long long)b * each + tid / threads; x < items; x += (long long)movers * each) {
       const long long rest = x / pieces;
       const int piece = (int)(x - rest * pieces), c = (int)(rest / moves), k = (int)(rest - (long long)c * moves);
       uint4* const cache = static_cast<uint4*>(list.cache[c]);
@@ -457,12 +458,12 @@ __global__ __launch_bounds__(kThreads) void k_pages_move(const PagesParams p, in
       uint4 v[kInFlight];
 #pragma unroll
       for (int u = 0; u < kInFlight; ++u) {
-        const int at = piece * kPiece + u * kThreads + tid;
+        const int at = piece * size + u * threads + lane;
         if (at < page) v[u] = p.keep_lines ? src[at] : load_stream16(&src[at]);
       }
 #pragma unroll
       for (int u = 0; u < kInFlight; ++u) {
-        const int at = piece * kPiece + u * kThreads + tid;
+        const int at = piece * size + u * threads + lane;
         if (at < page) store_stream16(&dst[at], v[u]);
       }
     }
