@@ -534,12 +534,11 @@ def _look(where: str, like, spec, *tensors):
 
 def _launch(fn, args, index: int, stream, where: str) -> None:
     """Launches on GPU `index`, which need not be the current one."""
+    args.stream = torch._C._cuda_getCurrentRawStream(index) if stream is None else int(stream.cuda_stream)
     if index == torch._C._cuda_getDevice():
-        args.stream = _stream_handle(stream)
         st = fn(args)
     else:
         with torch.cuda.device(index):
-            args.stream = _stream_handle(stream)
             st = fn(args)
     if st != HOOK_OK:
         raise HookError(st, where)
@@ -660,7 +659,7 @@ def _pages_data(where: str, a, caches, like, workspace, index: int, stream):
         a.num_kv_heads, a.row_bytes = shape[-3], shape[-1] * each[0].element_size()
         if stacked:
             n, step = shape[0], shape[1] * shape[2] * 16 * a.row_bytes
-            pointers = range(pointers[0], pointers[0] + n * step, step) if n else ()
+            pointers = range(pointers[0], pointers[0] + n * step, step) if n and step else ()
     array = (ctypes.c_void_p * (n or 1))(*pointers)
     a.num_caches, a.caches = n, array
     return array, workspace
