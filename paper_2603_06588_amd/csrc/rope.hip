@@ -3,8 +3,9 @@
 //
 // Bound by memory: every element is read once and written once (keys twice where both outputs are asked for).  The angles
 // of a token are the same in all its heads, so a workgroup takes a token, lets one wave compute its cosines and sines
-// once into shared memory (a lane per pair) while another finds the token's slot in the cache, and then walks the token's heads by units of two vectors of what one load carries: the two halves of as many pairs, or neighbouring
-// pairs in each.  The first units are requested before the angles are computed.
+// once into shared memory (a lane per pair) while another finds the token's slot in the cache, and then walks the token's heads
+// by units of two vectors of what one load carries: the two halves of as many pairs, or neighbouring pairs in each.  The
+// first units are requested before the angles are computed.
 // 16384 tokens of 64 query and 8 key and value heads of 128 into the cache: 120 us, 5.9 TB/s (two tokens to a workgroup 123, four 137;
 // threads 128 / 512: 127 / 139); 8000 tokens of 32 and 8: 40 us, neighbouring pairs 39, 8-bit cache 43.
 #include "../../include/hook_api.h"

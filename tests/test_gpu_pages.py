@@ -69,7 +69,7 @@ def check_table(got, rows, before=None):
         assert got[i][len(row):] == rest, i
 
 
-STATES = [(1, 1, 16, 3), (1, 4, 60, 9), (3, 8, 100, 20), (9, 40, 500, 60), (64, 30, 400, 200), (65, 1100, 17000, 50), (300, 20, 300, 900), (7, 2100, 30000, 2500), (900, 12, 150, 400), (3, 4500, 71000, 10)]
+STATES = [(1, 1, 16, 3), (1, 4, 60, 9), (3, 8, 100, 20), (9, 40, 500, 60), (64, 30, 400, 200), (65, 1100, 17000, 50), (300, 20, 300, 900), (7, 2100, 30000, 2500), (900, 12, 150, 400), (1500, 6, 80, 300), (3, 4500, 71000, 10)]
 
 
 @pytest.mark.parametrize("S,mb,most,spare", STATES)
@@ -106,6 +106,20 @@ def test_fork_of_bad_input_is_safe():
     status.zero_()
     binding.hook_pages_fork(ints([0]), ints([[1]]), ints([-4]), counts, out[:1, :1].contiguous(), lens_out[:1], status)
     assert int(lens_out[0]) == 0 and int(status) == G.BAD_LENGTH
+
+
+@pytest.mark.parametrize("S", [40, 1300])
+def test_fork_that_only_reorders(S):
+    """Every row goes on in another place: no count changes, and a row named twice counts once more."""
+    p = Pool(S, S, 10, 150, 50)
+    order = list(range(S))
+    random.Random(S).shuffle(order)
+    for src in (order, list(range(S)), order[:-1] + [order[0]]):
+        refs, out, lens, status = ints(p.refs), torch.full((S, 10), JUNK, dtype=torch.int32, device=DEV), ints([0] * S), ints([0])
+        binding.hook_pages_fork(ints(src), ints(p.table()), ints(p.lens), refs, out, lens, status)
+        rows, L, counts, bits = G.fork(src, p.table(), p.lens, p.refs)
+        check_table(out, rows)
+        assert lens.tolist() == L and refs.tolist() == counts and int(status) == bits == 0
 
 
 def test_fork_from_and_to_no_rows():
