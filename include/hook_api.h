@@ -497,8 +497,8 @@ hook_status hook_reduce_mass(const hook_reduce_args* args);
  * With k_cache and v_cache given, the call also does what hook_kv_write would do with the rotated keys and with v:
  * the rows go to the slots of the batch's new tokens (num_tokens = cu_q_lens[num_seqs]), bit for bit as by the two calls,
  * quantised for an 8-bit cache; tokens are dropped by the same rules.  k_out may then be null (the keys go to the cache alone).
- * Any head_dim up to HOOK_ROPE_MAX_DIM and any even rotary_dim; rows, halves and pointers that are multiples of 16 bytes run at
- * full speed, others with loads of the largest power of two that divides them (of single elements: half of it).  Pointers are aligned to their elements.
+ * Any head_dim up to HOOK_ROPE_MAX_DIM and any even rotary_dim; heads, halves of what turns, strides and pointers that are multiples of
+ * 16 bytes (a cache of 8 bits: 8) run at full speed, others at about 60 % of it.  Pointers are aligned to their elements.
  */
 #define HOOK_ROPE_MAX_AXES 4
 #define HOOK_ROPE_MAX_DIM 512

@@ -20,6 +20,7 @@ constexpr int kRopeInFlight = 2;      // units that a thread requests together (
 struct RopeParams {
   int T, Hq, Hk, Hv, d, pairs;        // Hk, Hv: 0 where k is not rotated, or no cache is written
   int axes, axis_pairs[HOOK_ROPE_MAX_AXES], cyclic;
+  int q_apart, k_apart;               // the output is not the input
   float magnitude, sign;
   const int* positions;
   const float* inv_freq;
@@ -33,49 +34,70 @@ struct RopeParams {
   const float *k_scale, *v_scale;
 };
 
-template <int BYTES> struct RawOf;
-template <> struct RawOf<16> { typedef u32x4 type; };
-template <> struct RawOf<8> { typedef u32x2 type; };
-template <> struct RawOf<4> { typedef unsigned int type; };
-template <> struct RawOf<2> { typedef unsigned short type; };
-template <> struct RawOf<1> { typedef unsigned char type; };
-
 template <typename E, int W> struct Vec {
   E e[W];
 };
 
-template <typename E, int W>
-__device__ __forceinline__ Vec<E, W> load_vec(const char* p) {
-  typedef typename RawOf<sizeof(E) * W>::type Raw;
-  const Raw r = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(p));
+// W elements at an address that is a multiple of 16 bytes (ALIGNED), or of one element alone.
+template <typename E, int W, bool ALIGNED> struct RawOf {
+  typedef unsigned int type __attribute__((ext_vector_type(sizeof(E) * W / 4), aligned(ALIGNED ? sizeof(E) * W : sizeof(E))));
+};
+
+// The first n of W elements (all of them where ALIGNED).
+template <typename E, int W, bool ALIGNED>
+__device__ __forceinline__ Vec<E, W> load_vec(const char* p, int n) {
+  typedef typename RawOf<E, W, ALIGNED>::type Raw;
   Vec<E, W> v;
-  __builtin_memcpy(&v, &r, sizeof v);
+  if (ALIGNED || n == W) {
+    const Raw r = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(p));
+    __builtin_memcpy(&v, &r, sizeof v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j) v.e[j] = j < n ? reinterpret_cast<const E*>(p)[j] : (E)0.0f;
+  }
   return v;
 }
 
-template <typename E, int W>
-__device__ __forceinline__ void store_vec(char* p, const Vec<E, W>& v) {
-  typedef typename RawOf<sizeof(E) * W>::type Raw;
-  Raw r;
-  __builtin_memcpy(&r, &v, sizeof r);
-  __builtin_nontemporal_store(r, reinterpret_cast<Raw*>(p));
+template <typename E, int W, bool ALIGNED>
+__device__ __forceinline__ void store_vec(char* p, const Vec<E, W>& v, int n) {
+  typedef typename RawOf<E, W, ALIGNED>::type Raw;
+  if (ALIGNED || n == W) {
+    Raw r;
+    __builtin_memcpy(&r, &v, sizeof v);
+    if (ALIGNED) __builtin_nontemporal_store(r, reinterpret_cast<Raw*>(p));      // (parts of lines are to meet in the cache: 68 us -> 63)
+    else *reinterpret_cast<Raw*>(p) = r;
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (j < n) reinterpret_cast<E*>(p)[j] = v.e[j];
+  }
 }
 
-// W values as E4M3 bytes: what the cache write stores for them (kv_write_device.h)
-template <typename E, int W>
-__device__ __forceinline__ void store_e4m3(char* p, const Vec<E, W>& v, float scale) {
-  Vec<unsigned char, W> b;
-#pragma unroll
-  for (int i = 0; i < W; i += 2) {
-    const float lo = fp8_prescale((float)v.e[i], scale), hi = W > 1 ? fp8_prescale((float)v.e[W > 1 ? i + 1 : 0], scale) : 0.0f;
-    const int two = __builtin_amdgcn_cvt_pk_fp8_f32(lo, hi, 0, false);
-    b.e[i] = (unsigned char)(two & 0xFF);
-    if constexpr (W > 1) b.e[i + 1] = (unsigned char)((two >> 8) & 0xFF);
-  }
-  typedef typename RawOf<W>::type Raw;
+// The same as E4M3 bytes: what the cache write stores for them (kv_write_device.h)
+template <typename E, int W, bool ALIGNED>
+__device__ __forceinline__ void store_e4m3(char* p, const Vec<E, W>& v, float scale, int n) {
+  typedef unsigned int Raw __attribute__((ext_vector_type(W / 4), aligned(ALIGNED ? W : 1)));
   Raw r;
-  __builtin_memcpy(&r, &b, sizeof r);
-  *reinterpret_cast<Raw*>(p) = r;
+#pragma unroll
+  for (int i = 0; i < W / 4; ++i) {
+    int four = 0;
+    four = __builtin_amdgcn_cvt_pk_fp8_f32(fp8_prescale((float)v.e[4 * i], scale), fp8_prescale((float)v.e[4 * i + 1], scale), four, false);
+    four = __builtin_amdgcn_cvt_pk_fp8_f32(fp8_prescale((float)v.e[4 * i + 2], scale), fp8_prescale((float)v.e[4 * i + 3], scale), four, true);
+    r[i] = (unsigned)four;
+  }
+  if (ALIGNED || n == W) {
+    *reinterpret_cast<Raw*>(p) = r;
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (j < n) p[j] = (char)(r[j / 4] >> (8 * (j % 4)));
+  }
+}
+
+// Units of a head: the turned pairs, then the rest of it, two vectors at a time.
+__host__ __device__ __forceinline__ int vectors_of(int elements, int width) { return (elements + width - 1) / width; }
+__host__ __device__ __forceinline__ int units_of(int d, int pairs, int width, bool neighbours) {
+  return neighbours ? (vectors_of(d, width) + 1) / 2 : vectors_of(pairs, width) + (vectors_of(d - 2 * pairs, width) + 1) / 2;
 }
 
 // Largest i in [0, n) with cu[i] <= row, by all lanes of a wave: each trip to memory leaves one 64th of the sequences.
@@ -91,38 +113,63 @@ __device__ __forceinline__ int find_sequence(const int* cu, int n, int row, int 
   return lo;
 }
 
-template <typename E, int W, bool NEIGHBOURS>
+// ALIGNED: pairs and heads are whole vectors, and every vector lies at a multiple of 16 bytes.  Otherwise vectors lie anywhere (the
+// memory takes them at any address) and the last one of the pairs, of what is behind them and of a head may be a part of one.  Such a
+// part is moved back to be a whole one, whose first elements another thread computes alike, unless those are turned in place or
+// there are not as many (8000 tokens of 32 + 8 heads with 25 pairs, halves: 63 us, 87 with parts by elements;
+// neighbours 51).
+template <typename E, int W, bool NEIGHBOURS, bool ALIGNED>
 __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int parts) {
   __shared__ float sh_cos[HOOK_ROPE_MAX_DIM / 2], sh_sin[HOOK_ROPE_MAX_DIM / 2];
   __shared__ long long sh_row;        // blk * Hkv * 16 + slot of the token in the cache, or -1
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int t = blockIdx.x / parts, part = blockIdx.x - t * parts;
-  const int units = (p.d + 2 * W - 1) / (2 * W);                // of a head: the turned ones, then the rest of it
-  const int total = (p.Hq + p.Hk + p.Hv) * units;
-  const int turned = p.pairs / W;
+  const int units = units_of(p.d, p.pairs, W, NEIGHBOURS), value_units = (vectors_of(p.d, W) + 1) / 2;
+  const int turning = (p.Hq + p.Hk) * units, total = turning + p.Hv * value_units;
 
   Vec<E, W> x[kRopeInFlight][2];
-  // where unit e of the token lies: head (queries, keys, values in a row) and the elements of its two vectors
-  struct Unit { int h, a, b; };                                 // b < 0: the head ends inside the unit
+  // where unit e of the token lies: head (queries, keys, values in a row), the elements that its two vectors begin with and how many
+  // of each there are; c is the first pair of a turned unit of halves
+  struct Unit { int h, a, b, n, m; bool turned; };
   auto unit = [&](int e) {
     Unit u;
-    u.h = e / units;
-    const int c = e - u.h * units;
-    // the unit's vectors lie apart rather than side by side, so that neighbouring lanes load neighbouring vectors
-    if (NEIGHBOURS && W == 1 && u.h < p.Hq + p.Hk) {
-      u.a = 2 * c;
-      u.b = u.a + 1;
-    } else if (NEIGHBOURS || u.h >= p.Hq + p.Hk) {
-      u.a = c * W;
-      u.b = (units + c) * W;
-    } else if (c < turned) {
-      u.a = c * W;
-      u.b = p.pairs + c * W;
-    } else {                                                    // behind both halves
-      u.a = (turned + c) * W;
-      u.b = (units + c) * W;
+    u.turned = false;
+    bool apart = true;
+    int c, lo = 0, half;              // unit of a part of the head that begins at lo and has its second vectors half of them further
+    if (e >= turning) {
+      u.h = p.Hq + p.Hk + (e - turning) / value_units;
+      c = (e - turning) % value_units;
+      half = value_units;
+    } else {
+      u.h = e / units;
+      c = e - u.h * units;
+      half = units;
+      apart = u.h < p.Hq ? p.q_apart : p.k_apart;
+      if (!NEIGHBOURS) {
+        const int turned = vectors_of(p.pairs, W);
+        if (c < turned) {
+          u.turned = true;
+          u.a = c * W;
+          if (!ALIGNED && apart && p.pairs >= W) u.a = min(u.a, p.pairs - W);
+          u.b = p.pairs + u.a;
+          u.n = u.m = ALIGNED ? W : min(W, p.pairs - u.a);
+          return u;
+        }
+        c -= turned;
+        half = units - turned;
+        lo = 2 * p.pairs;
+      }
     }
-    if (u.b + W > p.d) u.b = -1;
+    // the vectors lie apart rather than side by side, so that neighbouring lanes load neighbouring vectors
+    u.a = lo + c * W;
+    u.b = lo + (half + c) * W;
+    u.n = ALIGNED ? W : min(W, p.d - u.a);
+    u.m = ALIGNED ? (u.b < p.d ? W : 0) : max(0, min(W, p.d - u.b));
+    // (neighbouring pairs stay whole only where the head has an even number of elements)
+    if (!ALIGNED && apart && p.d - lo >= W && !(NEIGHBOURS && p.d % 2 != 0)) {
+      if (u.n < W) { u.a = p.d - W; u.n = W; }
+      if (u.m > 0 && u.m < W) { u.b = p.d - W; u.m = W; }
+    }
     return u;
   };
   auto request = [&](int e0) {
@@ -135,8 +182,8 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int p
       if (u.h < p.Hq) src = p.q + t * p.q_stride + (size_t)u.h * p.d * sizeof(E);
       else if (u.h < p.Hq + p.Hk) src = p.k + t * p.k_stride + (size_t)(u.h - p.Hq) * p.d * sizeof(E);
       else src = p.v + t * p.v_stride + (size_t)(u.h - p.Hq - p.Hk) * p.d * sizeof(E);
-      x[i][0] = load_vec<E, W>(src + (size_t)u.a * sizeof(E));
-      if (u.b >= 0) x[i][1] = load_vec<E, W>(src + (size_t)u.b * sizeof(E));
+      x[i][0] = load_vec<E, W, ALIGNED>(src + (size_t)u.a * sizeof(E), u.n);
+      if (u.m > 0) x[i][1] = load_vec<E, W, ALIGNED>(src + (size_t)u.b * sizeof(E), u.m);
     }
   };
   const int first = part * kRopeThreads + tid;
@@ -192,26 +239,26 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int p
         lo = (E)(a * cs - b * sn);
         hi = (E)(b * cs + a * sn);
       };
-      if (!value) {
-        if constexpr (NEIGHBOURS && W > 1) {
+      if constexpr (NEIGHBOURS) {
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int at = half == 0 ? u.a : u.b;
-            if (at < 0 || at >= 2 * p.pairs) continue;
+        for (int half = 0; half < 2; ++half) {
+          const int at = half == 0 ? u.a : u.b;
+          if (value || at >= 2 * p.pairs) continue;
 #pragma unroll
-            for (int j = 0; j < W; j += 2) turn(x[i][half].e[j], x[i][half].e[j + 1], (at + j) / 2);
-          }
-        } else if (NEIGHBOURS ? u.a < 2 * p.pairs : u.a < p.pairs) {
-#pragma unroll
-          for (int j = 0; j < W; ++j) turn(x[i][0].e[j], x[i][1].e[j], NEIGHBOURS ? u.a / 2 : u.a + j);
+          for (int j = 0; j < W; j += 2)
+            if (ALIGNED || at + j < 2 * p.pairs) turn(x[i][half].e[j], x[i][half].e[j + 1], (at + j) / 2);
         }
+      } else if (u.turned) {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+          if (ALIGNED || j < u.n) turn(x[i][0].e[j], x[i][1].e[j], u.a + j);
       }
       char* dst = nullptr;
       if (!value && !key) dst = p.q_out + t * p.q_out_stride + (size_t)u.h * p.d * sizeof(E);
       else if (key && p.k_out) dst = p.k_out + t * p.k_out_stride + (size_t)(u.h - p.Hq) * p.d * sizeof(E);
       if (dst) {
-        store_vec<E, W>(dst + (size_t)u.a * sizeof(E), x[i][0]);
-        if (u.b >= 0) store_vec<E, W>(dst + (size_t)u.b * sizeof(E), x[i][1]);
+        store_vec<E, W, ALIGNED>(dst + (size_t)u.a * sizeof(E), x[i][0], u.n);
+        if (u.m > 0) store_vec<E, W, ALIGNED>(dst + (size_t)u.b * sizeof(E), x[i][1], u.m);
       }
       if (p.Hv > 0 && (value || key) && sh_row >= 0) {
         const int g = value ? u.h - p.Hq - p.Hk : u.h - p.Hq;
@@ -219,35 +266,32 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int p
         char* cache = value ? p.v_cache : p.k_cache;
         if (p.kv8) {
           const float scale = value ? p.v_scale[g] : p.k_scale[g];
-          store_e4m3<E, W>(cache + row + u.a, x[i][0], scale);
-          if (u.b >= 0) store_e4m3<E, W>(cache + row + u.b, x[i][1], scale);
+          store_e4m3<E, W, ALIGNED>(cache + row + u.a, x[i][0], scale, u.n);
+          if (u.m > 0) store_e4m3<E, W, ALIGNED>(cache + row + u.b, x[i][1], scale, u.m);
         } else {
-          store_vec<E, W>(cache + (row + u.a) * sizeof(E), x[i][0]);
-          if (u.b >= 0) store_vec<E, W>(cache + (row + u.b) * sizeof(E), x[i][1]);
+          store_vec<E, W, ALIGNED>(cache + (row + u.a) * sizeof(E), x[i][0], u.n);
+          if (u.m > 0) store_vec<E, W, ALIGNED>(cache + (row + u.b) * sizeof(E), x[i][1], u.m);
         }
       }
     }
   }
 }
 
-template <typename E, int W, bool NEIGHBOURS>
-hipError_t launch_width(const RopeParams& p, hipStream_t st) {
-  const int units = (p.d + 2 * W - 1) / (2 * W);
-  const long long per_token = (long long)(p.Hq + p.Hk + p.Hv) * units;
+template <typename E, bool NEIGHBOURS, bool ALIGNED>
+hipError_t launch_rope(const RopeParams& p, hipStream_t st) {
+  constexpr int W = 16 / sizeof(E);
+  const long long per_token = (long long)(p.Hq + p.Hk) * units_of(p.d, p.pairs, W, NEIGHBOURS) + (long long)p.Hv * ((vectors_of(p.d, W) + 1) / 2);
   // Few tokens: a token's heads are cut over several workgroups, one round of units each, to be spread over the chip (2000 tokens of 32 and
   // 8 heads 14.8 us so, 12.0 with a workgroup each; 1000 tokens 8.5 with either, where the launch counts).
-  const int parts = p.T >= 600 ? 1 : (int)((per_token + kRopeThreads - 1) / kRopeThreads);
-  hipLaunchKernelGGL((k_rope<E, W, NEIGHBOURS>), dim3((unsigned)(p.T * parts)), dim3(kRopeThreads), 0, st, p, parts);
+  const long long parts = p.T >= 600 ? 1 : (per_token + kRopeThreads - 1) / kRopeThreads;
+  hipLaunchKernelGGL((k_rope<E, W, NEIGHBOURS, ALIGNED>), dim3((unsigned)(p.T * parts)), dim3(kRopeThreads), 0, st, p, (int)parts);
   return hipGetLastError();
 }
 
-template <typename E, bool NEIGHBOURS>
-hipError_t launch_rope(const RopeParams& p, int width, hipStream_t st) {
-  if constexpr (sizeof(E) == 2)
-    if (width == 8) return launch_width<E, 8, NEIGHBOURS>(p, st);
-  if (width >= 4) return launch_width<E, 4, NEIGHBOURS>(p, st);
-  if (width == 2) return launch_width<E, 2, NEIGHBOURS>(p, st);
-  return launch_width<E, 1, NEIGHBOURS>(p, st);
+template <typename E>
+hipError_t launch_rope(const RopeParams& p, bool neighbours, bool aligned, hipStream_t st) {
+  if (neighbours) return aligned ? launch_rope<E, true, true>(p, st) : launch_rope<E, true, false>(p, st);
+  return aligned ? launch_rope<E, false, true>(p, st) : launch_rope<E, false, false>(p, st);
 }
 
 }  // namespace
@@ -311,6 +355,8 @@ extern "C" hook_status hook_rope(const hook_rope_args* a) {
   p.axes = a->num_axes;
   for (int i = 0; i < a->num_axes; ++i) p.axis_pairs[i] = a->axis_pairs[i];
   p.cyclic = a->axis_order == HOOK_ROPE_CYCLIC;
+  p.q_apart = a->q_out != a->q;
+  p.k_apart = a->k_out != a->k;
   p.magnitude = a->magnitude != 0.0f ? a->magnitude : 1.0f;
   p.sign = a->inverse ? -p.magnitude : p.magnitude;
   p.positions = a->positions;
@@ -328,9 +374,8 @@ extern "C" hook_status hook_rope(const hook_rope_args* a) {
     p.k_cache = static_cast<char*>(a->k_cache); p.v_cache = static_cast<char*>(a->v_cache);
     p.k_scale = a->k_scale; p.v_scale = a->v_scale;
   }
-  // Elements that one load carries: the largest power of two, up to 16 bytes, that divides heads, pairs, strides and addresses
-  // (an 8-bit cache's rows are addressed by single bytes, so by elements).
-  uintptr_t grain = 16;
+  // Whether heads, halves, strides and addresses are all multiples of 16 bytes (of 8 in an 8-bit cache, whose rows take half of that).
+  uintptr_t grain = 0;
   auto divides = [&](uintptr_t bytes) { grain |= bytes; };
   divides((uintptr_t)a->head_dim * esize);
   divides((uintptr_t)pairs * esize);
@@ -346,14 +391,13 @@ extern "C" hook_status hook_rope(const hook_rope_args* a) {
     divides((uintptr_t)a->k_cache * (kv8 ? 2 : 1));
     divides((uintptr_t)a->v_cache * (kv8 ? 2 : 1));
   }
-  const int bytes = (int)(grain & (~grain + 1));
-  if (bytes < esize) return HOOK_ERR_UNSUPPORTED;
-  const int width = bytes / esize;
-  const long long units = (a->head_dim + 2 * width - 1) / (2 * width), per_token = (p.Hq + p.Hk + p.Hv) * units;
-  if (per_token > (1 << 27) || !grid_fits((per_token / kRopeThreads + 1) * p.T)) return HOOK_ERR_UNSUPPORTED;
+  if (grain % esize != 0) return HOOK_ERR_UNSUPPORTED;
+  // (an upper bound of the units of a token: one to a vector)
+  if (!grid_fits(((long long)(p.Hq + p.Hk + p.Hv) * (a->head_dim * esize / 16 + 3) / kRopeThreads + 1) * (p.T < 600 ? p.T : 1)) ||
+      (long long)(p.Hq + p.Hk + p.Hv) * (a->head_dim * esize / 16 + 3) > (1 << 27))
+    return HOOK_ERR_UNSUPPORTED;
   hipStream_t st = static_cast<hipStream_t>(a->stream);
-  const bool nb = a->layout == HOOK_ROPE_NEIGHBOURS;
-  const hipError_t e = a->dtype == HOOK_BF16 ? (nb ? launch_rope<__bf16, true>(p, width, st) : launch_rope<__bf16, false>(p, width, st))
-                                             : (nb ? launch_rope<float, true>(p, width, st) : launch_rope<float, false>(p, width, st));
+  const bool neighbours = a->layout == HOOK_ROPE_NEIGHBOURS, aligned = grain % 16 == 0;
+  const hipError_t e = a->dtype == HOOK_BF16 ? launch_rope<__bf16>(p, neighbours, aligned, st) : launch_rope<float>(p, neighbours, aligned, st);
   return e == hipSuccess ? HOOK_OK : HOOK_ERR_LAUNCH;
 }

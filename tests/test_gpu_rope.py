@@ -41,7 +41,8 @@ def inputs(T, hq, hkv, d, dtype, seed=0, far=1000, axes=1):
 
 
 @pytest.mark.parametrize("T,hq,hkv,d,r", [(1, 1, 1, 64, 64), (3, 32, 8, 128, 128), (17, 6, 2, 128, 64), (5, 5, 1, 80, 80), (2, 3, 3, 80, 48), (9, 2, 1, 72, 36),
-                                          (4, 2, 2, 6, 2), (7, 1, 1, 10, 10), (2, 1, 1, 512, 512), (33, 4, 4, 64, 0), (6, 2, 1, 13, 4), (130, 16, 2, 128, 128)])
+                                          (4, 2, 2, 6, 2), (7, 1, 1, 10, 10), (2, 1, 1, 512, 512), (33, 4, 4, 64, 0), (6, 2, 1, 13, 4), (130, 16, 2, 128, 128),
+                                          (700, 3, 2, 128, 50), (650, 2, 1, 96, 94), (3, 9, 3, 33, 32), (5, 1, 1, 127, 126), (2, 2, 2, 24, 20)])
 @pytest.mark.parametrize("neighbours", [False, True])
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_against_the_definition(T, hq, hkv, d, r, neighbours, dtype):
@@ -53,6 +54,10 @@ def test_against_the_definition(T, hq, hkv, d, r, neighbours, dtype):
     for got, x in ((q_out, q), (k_out, k)):
         check(got, x, G.rope(x, pos, f, neighbours=neighbours), r, neighbours=neighbours)
         assert torch.equal(bits(got[..., r:]), bits(x[..., r:]))
+    # the same bits in place
+    qi, ki = q.to(DEV), k.to(DEV)
+    binding.hook_rope(qi, ki, pos.to(DEV), f.to(DEV), layout=int(neighbours))
+    assert torch.equal(bits(qi), bits(q_out)) and torch.equal(bits(ki), bits(k_out))
 
 
 @pytest.mark.parametrize("axes,sections,cyclic", [(1, (32,), True), (2, (20, 12), False), (3, (12, 10, 10), True), (3, (8, 12, 12), False),
@@ -169,11 +174,27 @@ def test_cache_write_is_that_of_the_two_calls(kind, new, prior):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "kv8"])
-@pytest.mark.parametrize("d,r", [(80, 40), (64, 20), (128, 6)])
-def test_cache_write_of_narrow_units(kind, d, r):
+@pytest.mark.parametrize("d,r", [(80, 40), (64, 20), (128, 6), (128, 50), (48, 34), (16, 14)])
+@pytest.mark.parametrize("layout", [binding.ROPE_HALVES, binding.ROPE_NEIGHBOURS])
+def test_cache_write_of_odd_units(kind, d, r, layout):
     table, lens, cu, blocks = batch([4, 9], [14, 7])
     q, k, v, pos = inputs(13, 3, 1, d, BF, seed=d)
-    fused_and_apart(q, k, v, pos, freqs(r), table, lens, cu, blocks, kind == "kv8", layout=binding.ROPE_NEIGHBOURS)
+    fused_and_apart(q, k, v, pos, freqs(r), table, lens, cu, blocks, kind == "kv8", layout=layout)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "kv8"])
+def test_cache_write_while_keys_turn_in_place(kind):
+    """k_out is k: the keys in the cache are those of the two calls, with whole vectors and with parts of one."""
+    for d, r in ((64, 64), (64, 38)):
+        table, lens, cu, blocks = batch([3, 5], [20, 2])
+        q, k, v, pos = (t.to(DEV) for t in inputs(8, 4, 2, d, BF, seed=r))
+        f, args = freqs(r).to(DEV), [t.to(DEV) for t in (table, lens, cu)]
+        caches = torch.zeros((2, 2, blocks, 2, 16, d), dtype=torch.uint8 if kind == "kv8" else BF, device=DEV)
+        scales = {"k_scale": torch.full((2,), 0.01, device=DEV), "v_scale": torch.full((2,), 0.02, device=DEV)} if kind == "kv8" else {}
+        want_q, want_k = binding.hook_rope(q, k, pos, f, q_out=torch.empty_like(q), k_out=torch.empty_like(k))
+        binding.hook_kv_write(want_k, v, *args, caches[0, 0], caches[0, 1], **scales)
+        binding.hook_rope(q, k, pos, f, k_out=k, v=v, block_table=args[0], seq_lens=args[1], cu_q_lens=args[2], k_cache=caches[1, 0], v_cache=caches[1, 1], **scales)
+        assert torch.equal(bits(q), bits(want_q)) and torch.equal(bits(k), bits(want_k)) and torch.equal(caches[0].view(torch.uint8), caches[1].view(torch.uint8))
 
 
 def test_cache_write_drops_what_the_cache_write_drops():
