@@ -626,7 +626,7 @@ hook_status hook_pages_compact(const hook_pages_args* args);
  * A token that none of these touches is copied bit for bit.  A mask that allows nothing leaves a row of -infinity.  Tokens outside [0, vocab) in
  * the lists are ignored.  Arrays that are null have no effect (repetition 1, frequency 0, presence 0, no bias, no mask,
  * prompt_lens 0: all of the history was generated).  Row i's history is history[cu_history[i] .. cu_history[i + 1] - 1], its bias
- * list likewise, both cut to the lengths given.  Its mask is row mask_rows[i] of `mask` (row i where mask_rows is null); outside
+ * list likewise, both cut to the lengths given (at most 2^30).  Its mask is row mask_rows[i] of `mask` (row i where mask_rows is null); outside
  * [0, num_masks): no mask.  `out` may be `logits` (same stride); otherwise the two share no element.
  */
 typedef struct hook_steer_logits_args {

@@ -248,6 +248,7 @@ extern "C" hook_status hook_steer_logits(const hook_steer_logits_args* a) {
   if (a->num_rows < 0 || a->vocab < 0 || a->logits_stride < 0 || a->out_stride < 0 || a->history_len < 0 || a->bias_len < 0 || a->num_masks < 0)
     return HOOK_ERR_SHAPE;
   if (a->dtype != HOOK_BF16 && a->dtype != HOOK_F32) return HOOK_ERR_UNSUPPORTED;
+  if (a->history_len > (1 << 30) || a->bias_len > (1 << 30)) return HOOK_ERR_UNSUPPORTED;      // (entries are counted on past the end)
   if (a->vocab > (1 << 30) || !grid_fits(((long long)a->num_rows + 8) * (a->vocab / 8192 + 2))) return HOOK_ERR_UNSUPPORTED;
   if (a->num_rows == 0 || a->vocab == 0) return HOOK_OK;
   const long long stride = a->logits_stride ? a->logits_stride : a->vocab, out_stride = a->out_stride ? a->out_stride : a->vocab;

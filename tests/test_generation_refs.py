@@ -247,6 +247,8 @@ def test_logits_refusals(binding):
     assert _logits(binding, logits_stride=99) == 2 and _logits(binding, out_stride=99) == 2
     assert _logits(binding, logits_stride=104) == 2                               # its own input at another stride
     assert _logits(binding, logits_stride=1 << 41, out=2 * P) == 3
+    assert _logits(binding, history_len=(1 << 30) + 1, history=P, cu_history=P) == 3
+    assert _logits(binding, bias_len=(1 << 30) + 1, cu_bias=P, bias_ids=P, bias_values=P) == 3
     assert _logits(binding, logits=0) == 1 and _logits(binding, out=0) == 1
     assert _logits(binding, history_len=5, history=P) == 1 and _logits(binding, history_len=5, cu_history=P) == 1
     assert _logits(binding, bias_len=5, cu_bias=P, bias_ids=P) == 1
