@@ -624,6 +624,8 @@ def _pages_args(where: str, block_table, seq_lens, ref_counts, table_out, lens_o
         raise HookError(2, f"{where} (block_table: shape)")
     num_seqs, max_blocks = block_table.shape
     new_rows = num_seqs if src_rows is None else rows
+    if table_out is not None and (table_out.dim() != 2 or table_out.shape[1] != max_blocks):
+        raise HookError(2, f"{where} (block_table_out: shape)")
     if (nlens != num_seqs or nst != 1 or nrefs != num_blocks or nto != new_rows * max_blocks or nlens_to != new_rows or
             (src_lens is not None and ncut != rows) or (cu_q_lens is not None and ncu != num_seqs + 1) or
             (page_map is not None and (npm != num_blocks or nlive != 1))):

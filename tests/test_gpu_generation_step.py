@@ -113,3 +113,43 @@ def test_steps(seed):
         fine = torch.isfinite(w)
         assert torch.equal(torch.isneginf(y.cpu().double()), ~fine)
         assert float(((y.cpu().double() - w).abs() - slack - 2.0 ** -8 * (w.abs() + slack))[fine].max()) <= 0
+
+
+def test_host_threads_on_streams_of_their_own():
+    """Three threads make the calls at once, each on its own stream with its own tensors."""
+    import threading
+    from test_gpu_pages import Pool, check_table, new_caches, run_append
+    done, failed = [], []
+
+    def job(seed):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                p = Pool(seed, 40, 12, 150, 200, share=0.8)
+                start, status, cu = new_caches(p.nb, 2, 16, torch.bfloat16, 4, seed), ints([0]), list(range(41))
+                x = torch.randn((9, 5000), device=DEV, generator=torch.Generator(DEV).manual_seed(seed)).bfloat16()
+                h, cu_h = ints([(7 * seed + t) % 5000 for t in range(900)]), ints(list(range(0, 901, 100)))
+                for _ in range(20):
+                    caches = start.clone()
+                    table, lens, refs = run_append(p, cu, caches, True, status)
+                    y = binding.hook_steer_logits(x, out=torch.empty_like(x), history=h, cu_history=cu_h, presence=torch.ones(9, device=DEV))
+                stream.synchronize()
+                rows, L, counts, copies, _ = G.append(cu, p.table(), p.lens, p.refs)
+                check_table(table, rows)
+                for a, b, n in copies:
+                    start[:, b, :, :n] = start[:, a, :, :n]
+                assert lens.tolist() == L and refs.tolist() == counts and torch.equal(caches, start)
+                want = x.clone()
+                at = torch.arange(9, device=DEV).repeat_interleave(100), h.long()
+                want[at] = (x[at].float() - 1).bfloat16()
+                assert torch.equal(bits(y), bits(want))
+            done.append(seed)
+        except BaseException as e:      # (pytest does not see other threads' errors)
+            failed.append(e)
+
+    threads = [threading.Thread(target=job, args=(k,)) for k in (1, 2, 3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed and sorted(done) == [1, 2, 3], failed

@@ -425,7 +425,7 @@ def test_refusals_of_the_binding():
     i, t = ints([0]), ints([[0, 0]])
     c = torch.zeros((1, 1, 16, 8), dtype=torch.bfloat16, device=DEV)
     fork = dict(src_rows=i, block_table=t, seq_lens=i, ref_counts=ints([0]), block_table_out=t.clone(), seq_lens_out=ints([0]), status=ints([0]))
-    for bad in (dict(src_rows=i.long()), dict(block_table_out=t), dict(seq_lens_out=i), dict(block_table_out=ints([[0]])), dict(status=ints([0, 0])), dict(src_lens=ints([1, 2])),
+    for bad in (dict(src_rows=i.long()), dict(block_table_out=t.view(2, 1).clone()), dict(block_table_out=t), dict(seq_lens_out=i), dict(block_table_out=ints([[0]])), dict(status=ints([0, 0])), dict(src_lens=ints([1, 2])),
                 dict(block_table=t.cpu()), dict(ref_counts_out=ints([0, 0]))):
         with pytest.raises(binding.HookError):
             binding.hook_pages_fork(**{**fork, **bad})
