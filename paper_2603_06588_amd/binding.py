@@ -7,6 +7,7 @@ built (``python -m paper_2603_06588_amd.build``).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -226,6 +227,15 @@ def _stream_handle(stream) -> int:
     if stream is None:      # the current stream's handle itself: building a Stream object takes ten times as long
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return int(stream.cuda_stream)
+
+
+_SAME = contextlib.nullcontext()
+
+
+def _taken_on(stream):
+    """Where a call on `stream` takes new memory from: that stream's own pool.  A block of another stream's may be one that has just been given
+    back there while work queued on it still uses the block, and nothing orders the call behind that work."""
+    return _SAME if stream is None else torch.cuda.stream(stream)
 
 
 class AttnProbeCall:
@@ -646,9 +656,8 @@ def _pages_data(where: str, a, caches, like, workspace, index: int, stream):
     if spec is None:
         spec = _CACHES[n] = tuple(f"ccaches[{i}]" for i in range(n)) + ("cworkspace",)
     if workspace is None:
-        workspace = torch.empty(pages_workspace_bytes(a.num_seqs, a.num_blocks), dtype=torch.uint8, device=index)
-        if stream is not None:
-            workspace.record_stream(stream)
+        with _taken_on(stream):
+            workspace = torch.empty(pages_workspace_bytes(a.num_seqs, a.num_blocks), dtype=torch.uint8, device=index)
     seen = _look(where, like, spec, *each, workspace)
     a.workspace, a.workspace_bytes = seen[-2], workspace.numel() * workspace.element_size()
     pointers = seen[1:-2:2]

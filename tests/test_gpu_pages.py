@@ -438,3 +438,20 @@ def test_refusals_of_the_binding():
     for bad in (dict(page_map=ints([0, 0])), dict(num_live=ints([0, 0])), dict(block_table_out=ints([[0]]))):
         with pytest.raises(binding.HookError):
             binding.hook_pages_compact(**{**com, **bad})
+
+
+def test_scratch_of_a_call_on_another_stream_is_that_streams(monkeypatch):
+    """The call's own scratch is taken while the call's stream is the current one."""
+    p = Pool(41, 9, 12, 150, 60, share=0.8)
+    side, taken, empty = torch.cuda.Stream(), [], torch.empty
+    caches, status = new_caches(p.nb, 1, 16, torch.bfloat16, 2), ints([0])
+    t, L, c, page_map, live, cu = ints(p.table()), ints(p.lens), ints(p.refs), ints([0] * p.nb), ints([0]), ints(list(range(10)))
+    side.wait_stream(torch.cuda.current_stream())
+    monkeypatch.setattr(binding.torch, "empty", lambda *a, **kw: taken.append(torch.cuda.current_stream()) or empty(*a, **kw))
+    binding.hook_pages_append(cu, t, L, c, caches, status, stream=side)
+    binding.hook_pages_compact(t, L, c, caches, page_map, live, status, stream=side)
+    monkeypatch.undo()
+    side.synchronize()
+    assert taken == [side, side] and torch.cuda.current_stream() != side
+    rows, lens, counts, _, _ = G.append(list(range(10)), p.table(), p.lens, p.refs)
+    assert L.tolist() == lens and int(live) == sum(n > 0 for n in counts) and int(status) == 0

@@ -1,0 +1,85 @@
+"""Where the Python calls take memory from when they are given a stream: from that stream's pool, so that a block is never one that another
+stream has given back with work still queued on it.  The library and the streams are stand-ins here (no GPU)."""
+import types
+
+import pytest
+import torch
+
+from paper_2603_06588_amd import binding
+
+
+class Streams:
+    """The current stream's name, as torch.cuda.stream() switches it."""
+
+    def __init__(self):
+        self.current, self.taken, self.recorded = "current", [], []
+
+    def switch(self, stream):
+        outer = self
+
+        class Context:
+            def __enter__(self):
+                self.before, outer.current = outer.current, stream
+
+            def __exit__(self, *_):
+                outer.current = self.before
+        return Context()
+
+
+class Library:
+    """Accepts every call; any scratch is 512 bytes."""
+
+    def __getattr__(self, name):
+        return (lambda *a: 512) if name.endswith("_workspace_bytes") else (lambda *a: 0)
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    s = Streams()
+
+    def on_host(make):
+        def made(*args, **kw):
+            kw.pop("device", None)
+            t = make(*args, **kw)
+            s.taken.append((s.current, t))
+            return t
+        return made
+    monkeypatch.setattr(binding.torch, "empty", on_host(torch.empty))
+    monkeypatch.setattr(binding.torch, "empty_like", on_host(torch.empty_like))
+    monkeypatch.setattr(torch.cuda, "stream", s.switch)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: s.current)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: s.recorded.append((stream, t)))
+    monkeypatch.setattr(binding, "load_library", Library)
+    monkeypatch.setattr(binding, "pages_workspace_bytes", lambda *a: 512)
+    monkeypatch.setattr(binding, "_look", lambda where, like, spec, *tensors: (0,) + (0, ()) * len(tensors))
+    return s
+
+
+def calls():
+    i = lambda *n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    pages = binding.HookPagesArgs(1, 2, 4, 16)
+    return {
+        "hook_pages_append, hook_pages_compact": (lambda s: binding._pages_data("pages", pages, [], i(1, 2), None, 0, s) and (), 0, 1),
+    }
+
+
+@pytest.mark.parametrize("name", list(calls()))
+def test_memory_comes_from_the_stream_of_the_call(name, streams, monkeypatch):
+    call, results, allocations = calls()[name]
+    stream = types.SimpleNamespace(cuda_stream=77)
+    monkeypatch.setattr(binding, "_stream_handle", lambda s: 77)
+    out = call(stream)
+    assert len(streams.taken) == allocations and all(on is stream for on, _ in streams.taken)
+    # results outlive the call and are read on the current stream, scratch is not
+    assert len(out) == results and {id(t) for t in out} == {id(t) for _, t in streams.recorded}
+    assert all(on == "current" for on, _ in streams.recorded)
+
+
+@pytest.mark.parametrize("name", list(calls()))
+@pytest.mark.parametrize("given", [False, True])
+def test_calls_on_the_current_stream_record_nothing(name, given, streams, monkeypatch):
+    call, _, allocations = calls()[name]
+    streams.current = types.SimpleNamespace(cuda_stream=5) if given else "current"
+    monkeypatch.setattr(binding, "_stream_handle", lambda s: 5)
+    call(streams.current if given else None)
+    assert len(streams.taken) == allocations and all(on is streams.current for on, _ in streams.taken) and not streams.recorded
