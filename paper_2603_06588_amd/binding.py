@@ -238,11 +238,23 @@ def _taken_on(stream):
     return _SAME if stream is None else torch.cuda.stream(stream)
 
 
+def _handed_over(stream, *results):
+    """Results that a call on `stream` has taken memory for are read on the current stream (once the program has made it wait): their
+    memory is not given to anybody else before that is done."""
+    if stream is not None and results:
+        current = torch.cuda.current_stream(results[0].device)
+        if current != stream:
+            for t in results:
+                t.record_stream(current)
+
+
 class AttnProbeCall:
     """A marshalled ``hook_attn_probe`` call that can be launched repeatedly.
 
     Holds references to every tensor it points at, the output tensors and the
-    workspace, so relaunching costs one ctypes call and no allocation.
+    workspace, so relaunching costs one ctypes call and no allocation.  What it
+    allocates belongs to the stream that is current where it is made: a launch on
+    another stream waits for that one first, and the object outlives the launch.
     """
 
     def __init__(self, q, k_cache, v_cache, block_table, seq_lens, cu_q_lens, probe_heads=None, max_sel_q=1,
@@ -321,9 +333,11 @@ def hook_attn_probe(q, k_cache, v_cache, block_table, seq_lens, cu_q_lens, probe
                     query_sel=None, max_spans=1, key_spans=None, scale: float = 0.0,
                     stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(out, mass) of one layer's hooked attention; asynchronous on the current stream."""
-    call = AttnProbeCall(q, k_cache, v_cache, block_table, seq_lens, cu_q_lens, probe_heads, max_sel_q,
-                         query_sel, max_spans, key_spans, scale)
+    with _taken_on(stream):
+        call = AttnProbeCall(q, k_cache, v_cache, block_table, seq_lens, cu_q_lens, probe_heads, max_sel_q,
+                             query_sel, max_spans, key_spans, scale)
     call.launch(stream)
+    _handed_over(stream, call.out, call.mass)
     return call.out, call.mass
 
 
@@ -340,8 +354,11 @@ def hook_span_mass(q, k_cache, block_table, seq_lens, cu_q_lens, probe_heads, ma
     P = int(probe_heads.numel())
     if q.dtype not in _DT:
         raise HookError(3, "hook_span_mass (dtype)")
+    results = ()
     if mass is None:
-        mass = torch.empty((num_seqs, P, int(max_sel_q), int(max_spans)), dtype=torch.float32, device=q.device)
+        with _taken_on(stream):
+            mass = torch.empty((num_seqs, P, int(max_sel_q), int(max_spans)), dtype=torch.float32, device=q.device)
+        results = (mass,)
     a = HookAttnProbeArgs()
     a.num_seqs, a.total_q, a.num_q_heads, a.num_kv_heads = num_seqs, total_q, Hq, Hkv
     a.head_dim, a.block_size, a.max_blocks_per_seq, a.num_blocks = d, B, max_blocks, num_blocks
@@ -356,12 +373,14 @@ def hook_span_mass(q, k_cache, block_table, seq_lens, cu_q_lens, probe_heads, ma
         a.kv_dtype, a.k_scale = KV_FP8_E4M3, _p(k_scale)
     if workspace is None and use_workspace:
         need = int(lib.hook_span_mass_workspace_bytes(ctypes.byref(a)))
-        workspace = torch.empty(max(need, 8), dtype=torch.uint8, device=q.device) if need else None
+        with _taken_on(stream):
+            workspace = torch.empty(max(need, 8), dtype=torch.uint8, device=q.device) if need else None
     if workspace is not None:
         a.workspace, a.workspace_bytes = _p(workspace), workspace.numel()
     st = lib.hook_span_mass(ctypes.byref(a))
     if st != HOOK_OK:
         raise HookError(st, "hook_span_mass")
+    _handed_over(stream, *results)
     return mass
 
 
@@ -428,10 +447,14 @@ def hook_capture_qk(q, k_cache, block_table, seq_lens, cu_q_lens, probe_heads, m
     num_seqs, max_blocks = block_table.shape
     P = int(probe_heads.numel()) if probe_heads is not None else 0
     KH = int(capture_kv_heads.numel()) if capture_kv_heads is not None else 0
-    if q_out is None:
-        q_out = torch.empty((num_seqs, P, int(max_sel_q), d), dtype=q.dtype, device=q.device)
-    if k_out is None:
-        k_out = torch.empty((int(total_k), KH, d), dtype=k_cache.dtype, device=q.device)   # bytes for an 8-bit cache
+    results = []
+    with _taken_on(stream):
+        if q_out is None:
+            q_out = torch.empty((num_seqs, P, int(max_sel_q), d), dtype=q.dtype, device=q.device)
+            results.append(q_out)
+        if k_out is None:
+            k_out = torch.empty((int(total_k), KH, d), dtype=k_cache.dtype, device=q.device)   # bytes for an 8-bit cache
+            results.append(k_out)
     a = HookCaptureQkArgs()
     a.num_seqs, a.total_q, a.num_q_heads, a.num_kv_heads = num_seqs, total_q, Hq, Hkv
     a.head_dim, a.block_size, a.max_blocks_per_seq, a.num_blocks = d, B, max_blocks, num_blocks
@@ -446,6 +469,7 @@ def hook_capture_qk(q, k_cache, block_table, seq_lens, cu_q_lens, probe_heads, m
     st = lib.hook_capture_qk(ctypes.byref(a))
     if st != HOOK_OK:
         raise HookError(st, "hook_capture_qk")
+    _handed_over(stream, *results)
     return q_out, k_out
 
 
@@ -454,11 +478,14 @@ def hook_reduce_mass(mass, mode: int, span_a: int = 0, span_b: int = 1, query_se
     """Reduce mass [num_seqs, P, NQ, S] to scores ([num_seqs, S] for SPAN_MEAN, else [num_seqs])."""
     lib = load_library()
     num_seqs, P, NQ, S = mass.shape
+    results = ()
     if scores is None:
         if accumulate:
             raise ValueError("accumulate needs an existing scores tensor")
         shape = (num_seqs, S) if mode == REDUCE_SPAN_MEAN else (num_seqs,)
-        scores = torch.empty(shape, dtype=torch.float32, device=mass.device)
+        with _taken_on(stream):
+            scores = torch.empty(shape, dtype=torch.float32, device=mass.device)
+        results = (scores,)
     a = HookReduceArgs()
     a.num_seqs, a.num_probe_heads, a.max_sel_q, a.max_spans = num_seqs, P, NQ, S
     a.mass, a.query_sel, a.cu_q_lens, a.head_weights = _p(mass), _p(query_sel), _p(cu_q_lens), _p(head_weights)
@@ -467,6 +494,7 @@ def hook_reduce_mass(mass, mode: int, span_a: int = 0, span_b: int = 1, query_se
     st = lib.hook_reduce_mass(ctypes.byref(a))
     if st != HOOK_OK:
         raise HookError(st, "hook_reduce_mass")
+    _handed_over(stream, *results)
     return scores
 
 

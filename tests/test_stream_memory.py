@@ -56,9 +56,14 @@ def streams(monkeypatch):
 
 
 def calls():
-    i = lambda *n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    f, i = torch.zeros, lambda *n: torch.zeros(n, dtype=torch.int32)
+    q, cache = f(3, 2, 64), f(4, 1, 16, 64)
     pages = binding.HookPagesArgs(1, 2, 4, 16)
     return {
+        "hook_attn_probe": (lambda s: binding.hook_attn_probe(q, cache, cache, i(1, 2), i(1), i(2), probe_heads=i(1), stream=s), 2, 3),
+        "hook_span_mass": (lambda s: (binding.hook_span_mass(q, cache, i(1, 2), i(1), i(2), i(1), 1, i(1, 1), 2, i(1, 2, 2), stream=s),), 1, 2),
+        "hook_capture_qk": (lambda s: binding.hook_capture_qk(q, cache, i(1, 2), i(1), i(2), i(1), 1, i(1, 1), i(1), i(2), 5, stream=s), 2, 2),
+        "hook_reduce_mass": (lambda s: (binding.hook_reduce_mass(f(1, 2, 3, 4), 0, stream=s),), 1, 1),
         "hook_pages_append, hook_pages_compact": (lambda s: binding._pages_data("pages", pages, [], i(1, 2), None, 0, s) and (), 0, 1),
     }
 
