@@ -718,6 +718,8 @@ def hook_pages_fork(src_rows, block_table, seq_lens, ref_counts, block_table_out
     src_rows[j], or is empty where that is -1; reference counts follow (in place unless ref_counts_out is given).  Bits of PAGES_* are
     added to `status`."""
     where = "hook_pages_fork"
+    if src_rows is None or block_table_out is None or seq_lens_out is None:      # (a table of no rows is empty tensors)
+        raise HookError(1, "hook_pages_fork (src_rows, block_table_out, seq_lens_out)")
     a, index = _pages_args(where, block_table, seq_lens, ref_counts, block_table_out, seq_lens_out, ref_counts_out, status, src_rows, src_lens)
     _launch((_lib or load_library()).hook_pages_fork, a, index, stream, where)
 

@@ -455,3 +455,13 @@ def test_scratch_of_a_call_on_another_stream_is_that_streams(monkeypatch):
     assert taken == [side, side] and torch.cuda.current_stream() != side
     rows, lens, counts, _, _ = G.append(list(range(10)), p.table(), p.lens, p.refs)
     assert L.tolist() == lens and int(live) == sum(n > 0 for n in counts) and int(status) == 0
+
+
+@pytest.mark.parametrize("missing", ["src_rows", "block_table_out", "seq_lens_out"])
+def test_fork_without_its_tensors_is_refused(missing):
+    refs, table = ints([1, 1]), ints([[0], [1]])
+    args = dict(src_rows=ints([0, 1]), block_table=table, seq_lens=ints([9, 9]), ref_counts=refs, block_table_out=torch.empty_like(table),
+                seq_lens_out=ints([0, 0]), status=ints([0]))
+    with pytest.raises(binding.HookError) as e:
+        binding.hook_pages_fork(**{**args, missing: None})
+    assert e.value.status == 1 and refs.tolist() == [1, 1]
