@@ -595,6 +595,8 @@ def hook_rope(q, k, positions, inv_freq, axis_pairs=None, layout: int = ROPE_HAL
     go to the cache, as by ``hook_kv_write``; k itself is then left alone unless it is k_out.  Rows may be views into a wider
     buffer.  Returns (q_out, k_out)."""
     where = "hook_rope"
+    if positions is None or inv_freq is None:      # (a head of which nothing turns has an empty inv_freq)
+        raise HookError(1, "hook_rope (positions, inv_freq)")
     cached = k_cache is not None or v_cache is not None
     if q_out is None:
         q_out = q

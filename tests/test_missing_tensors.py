@@ -37,3 +37,14 @@ def test_fork(missing, no_launch):
     with pytest.raises(binding.HookError) as e:
         binding.hook_pages_fork(**{**args, missing: None})
     assert e.value.status == 1 and len(no_launch) == 1
+
+
+@pytest.mark.parametrize("missing", ["positions", "inv_freq"])
+def test_rope(missing, no_launch):
+    """Without frequencies nothing would turn, and the call would report that all is well."""
+    args = dict(q=torch.zeros(5, 2, 8), k=None, positions=ints(5), inv_freq=torch.ones(4))
+    binding.hook_rope(**args)
+    assert len(no_launch) == 1
+    with pytest.raises(binding.HookError) as e:
+        binding.hook_rope(**{**args, missing: None})
+    assert e.value.status == 1 and len(no_launch) == 1
