@@ -620,7 +620,8 @@ hook_status hook_pages_fork(const hook_pages_args* a) {
   if (!sizes_supported(a)) return HOOK_ERR_UNSUPPORTED;
   const long long chunks = row_chunks_of(a);
   if (a->num_rows > (1 << 26) || !grid_fits(a->num_rows * chunks + a->max_blocks_per_seq)) return HOOK_ERR_UNSUPPORTED;
-  if (a->num_rows == 0 && a->num_seqs == 0) return HOOK_OK;
+  const bool no_rows = a->num_rows == 0 && a->num_seqs == 0;
+  if (no_rows && a->ref_counts == a->ref_counts_out) return HOOK_OK;
   if (!a->ref_counts || !a->ref_counts_out || !a->status) return HOOK_ERR_NULL;
   if (a->num_seqs > 0 && (!a->block_table || !a->seq_lens)) return HOOK_ERR_NULL;
   if (a->num_rows > 0 && (!a->src_rows || !a->block_table_out || !a->seq_lens_out)) return HOOK_ERR_NULL;
@@ -636,6 +637,7 @@ hook_status hook_pages_fork(const hook_pages_args* a) {
     hipLaunchKernelGGL(k_pages_copy_counts, dim3((unsigned)((p.nb + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p.refs, p.refs_out, p.nb);
     if (hipGetLastError() != hipSuccess) return HOOK_ERR_LAUNCH;
   }
+  if (no_rows) return HOOK_OK;
   const int columns = (p.mb + kCols - 1) / kCols;
   const dim3 grid((unsigned)(p.rows * chunks + std::min(columns, kCounters)));
   if (columns > kCounters) hipLaunchKernelGGL(k_pages_fork<true>, grid, dim3(kForkThreads), 0, st, p, (int)chunks);

@@ -267,3 +267,10 @@ def test_binding_refuses_what_it_can_see(binding):
         binding.hook_pages_fork(i, i.view(1, 2), i[:1], i, i.view(2, 1), i, i[:1])
     with pytest.raises(binding.HookError):
         binding.hook_steer_logits(torch.zeros((2, 8)))
+
+
+def test_fork_of_no_rows_still_needs_both_counts(binding):
+    fork = binding.load_library().hook_pages_fork
+    none = dict(num_seqs=0, num_rows=0)
+    assert fork(_pages(binding, **none, ref_counts_out=0)) == 1 and fork(_pages(binding, **none, ref_counts=0)) == 1
+    assert fork(_pages(binding, **none, ref_counts=0, ref_counts_out=0)) == 0     # no counts that could change

@@ -465,3 +465,13 @@ def test_fork_without_its_tensors_is_refused(missing):
     with pytest.raises(binding.HookError) as e:
         binding.hook_pages_fork(**{**args, missing: None})
     assert e.value.status == 1 and refs.tolist() == [1, 1]
+
+
+@pytest.mark.parametrize("mb", [1, 5000])
+def test_fork_of_no_rows_into_no_rows_hands_the_counts_on(mb):
+    none, empty = torch.empty((0, mb), dtype=torch.int32, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV)
+    refs, counts, status = ints([3, 0, 1] * 100), ints([99] * 300), ints([0])
+    binding.hook_pages_fork(empty, none, empty, refs, none.clone(), empty.clone(), status, ref_counts_out=counts)
+    assert counts.tolist() == refs.tolist() == [3, 0, 1] * 100 and int(status) == 0
+    binding.hook_pages_fork(empty, none, empty, refs, none.clone(), empty.clone(), status)
+    assert refs.tolist() == [3, 0, 1] * 100 and int(status) == 0
