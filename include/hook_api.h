@@ -34,6 +34,8 @@
  *     bad table cannot fault, lengths beyond the table are clamped, and the
  *     condition is recorded in the workspace (see hook_attn_probe_device_status;
  *     hook_attn_probe_validate checks the contents on request).
+ *   - A launch takes fewer than 2^32 threads.  Sizes that need more (hook_rope: more than 2^24 - 1 tokens) are refused with
+ *     HOOK_ERR_UNSUPPORTED.
  *   - One call covers one layer; [layer, head] lists (Section 2, config example)
  *     are split per layer by the caller.
  */

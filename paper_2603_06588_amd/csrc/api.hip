@@ -252,8 +252,8 @@ __attribute__((visibility("hidden"))) hook_status run_attn_probe(const hook_attn
   const Layout l = make_layout(a, workspace_bytes);
   // one-dimensional launch grids over the item capacities
   if (a->dtype == HOOK_BF16 &&
-      (!grid_fits((long long)l.pf_cap * a->num_kv_heads * l.hgroups) ||
-       !grid_fits((long long)l.dec_cap * a->num_kv_heads * l.dec_hgroups)))
+      (!grid_fits((long long)l.pf_cap * a->num_kv_heads * l.hgroups, 64 * l.pf_waves) ||
+       !grid_fits((long long)l.dec_cap * a->num_kv_heads * l.dec_hgroups, 256)))
     return HOOK_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < l.needed || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0)
     return HOOK_ERR_WORKSPACE;

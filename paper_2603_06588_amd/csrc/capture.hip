@@ -142,7 +142,7 @@ extern "C" hook_status hook_capture_qk(const hook_capture_qk_args* a) {
   const long long chunks = (long long)p.num_seqs * p.P * p.NQ * p.row_chunks;
   if (do_q) {
     if (!a->q || !a->cu_q_lens || !a->probe_heads || !a->query_sel || !a->q_out) return HOOK_ERR_NULL;
-    if (!grid_fits((chunks + 255) / 256)) return HOOK_ERR_UNSUPPORTED;
+    if (!grid_fits((chunks + 255) / 256, 256)) return HOOK_ERR_UNSUPPORTED;
   }
   if (do_k) {
     if (!a->k_cache || !a->block_table || !a->seq_lens || !a->capture_kv_heads || !a->cu_k_lens || !a->k_out)

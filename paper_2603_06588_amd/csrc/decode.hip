@@ -214,7 +214,7 @@ template <int D, int HP>
 hipError_t launch_decode_dh(const AttnParams& p, hipStream_t st) {
   if (p.dec_ranges > 0) {
     const long long grid = (long long)p.dec_ranges * p.Hkv * p.dec_hgroups;
-    if (!grid_fits(grid)) return hipErrorInvalidValue;
+    if (!grid_fits(grid, 256)) return hipErrorInvalidValue;
     constexpr int kFew = kStreamSeqs / 64, kMany = kScanMaxSeqs / 64;
     const dim3 g((unsigned)grid);
     if (p.num_seqs > kStreamSeqs) {
@@ -231,7 +231,7 @@ hipError_t launch_decode_dh(const AttnParams& p, hipStream_t st) {
   }
   const long long grid = (long long)p.dec_cap * p.Hkv * p.dec_hgroups;
   if (grid <= 0) return hipSuccess;
-  if (!grid_fits(grid)) return hipErrorInvalidValue;
+  if (!grid_fits(grid, 256)) return hipErrorInvalidValue;
   if (p.kv8) hipLaunchKernelGGL((k_decode<D, HP, true>), dim3((unsigned)grid), dim3(256), 0, st, p);
   else hipLaunchKernelGGL((k_decode<D, HP, false>), dim3((unsigned)grid), dim3(256), 0, st, p);
   return hipGetLastError();

@@ -326,8 +326,10 @@ inline hipError_t raise_lds_limit_once(const void* kernel, int bytes, std::atomi
   return hipSuccess;
 }
 
-// Launch grids are one-dimensional and must fit the 31-bit limit.
-inline bool grid_fits(long long workgroups) { return workgroups >= 0 && workgroups <= 0x7fffffffLL; }
+// Launch grids are one-dimensional: a launch takes fewer than 2^31 workgroups and fewer than 2^32 threads in all.
+inline bool grid_fits(long long workgroups, int threads) {
+  return workgroups >= 0 && workgroups <= 0x7fffffffLL && workgroups * threads <= 0xffffffffLL;
+}
 
 hipError_t launch_plan(const AttnParams& p, hipStream_t st);
 hipError_t launch_kv_write(const KvWriteParams& p, hipStream_t st);

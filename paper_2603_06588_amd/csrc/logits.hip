@@ -230,13 +230,14 @@ __global__ __launch_bounds__(NT) void k_steer_logits(const LogitsParams p, int r
 }
 
 template <typename E, int W, int NT, int VPT>
-hipError_t launch_range(const LogitsParams& p, hipStream_t st) {
+hook_status launch_range(const LogitsParams& p, hipStream_t st) {
   const bool on_border = (reinterpret_cast<uintptr_t>(p.logits) | (uintptr_t)p.stride) % 16 == 0;      // else a row may begin W - 1 elements behind one
   const int ranges = (p.V + (on_border ? 0 : W - 1) + NT * VPT * W - 1) / (NT * VPT * W);
   const int turn = p.R >= 8 ? 3 : 0;
-  const dim3 grid((unsigned)(((p.R + (1 << turn) - 1) >> turn << turn) * ranges));
-  hipLaunchKernelGGL((k_steer_logits<E, W, NT, VPT>), grid, dim3(NT), 0, st, p, ranges, turn);
-  return hipGetLastError();
+  const long long workgroups = (((long long)p.R + (1 << turn) - 1) >> turn << turn) * ranges;
+  if (!grid_fits(workgroups, NT)) return HOOK_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((k_steer_logits<E, W, NT, VPT>), dim3((unsigned)workgroups), dim3(NT), 0, st, p, ranges, turn);
+  return hipGetLastError() == hipSuccess ? HOOK_OK : HOOK_ERR_LAUNCH;
 }
 
 }  // namespace
@@ -249,7 +250,7 @@ extern "C" hook_status hook_steer_logits(const hook_steer_logits_args* a) {
     return HOOK_ERR_SHAPE;
   if (a->dtype != HOOK_BF16 && a->dtype != HOOK_F32) return HOOK_ERR_UNSUPPORTED;
   if (a->history_len > (1 << 30) || a->bias_len > (1 << 30)) return HOOK_ERR_UNSUPPORTED;      // (entries are counted on past the end)
-  if (a->vocab > (1 << 30) || !grid_fits(((long long)a->num_rows + 8) * (a->vocab / 8192 + 2))) return HOOK_ERR_UNSUPPORTED;
+  if (a->vocab > (1 << 30)) return HOOK_ERR_UNSUPPORTED;
   if (a->num_rows == 0 || a->vocab == 0) return HOOK_OK;
   const long long stride = a->logits_stride ? a->logits_stride : a->vocab, out_stride = a->out_stride ? a->out_stride : a->vocab;
   if (stride > (1ll << 40) || out_stride > (1ll << 40)) return HOOK_ERR_UNSUPPORTED;
@@ -277,8 +278,6 @@ extern "C" hook_status hook_steer_logits(const hook_steer_logits_args* a) {
   // (ranges of 16384 and 8192 tokens) against 256 and 512: 256 x 131072 bf16 36, 49 and 39 us, 128 x 131072 fp32 33, 46 and 38; four
   // rows 6 us with each of them.
   const bool wide = from % 16 == to % 16 && (uintptr_t)stride * esize % 16 == (uintptr_t)out_stride * esize % 16;
-  hipError_t e;
-  if (esize == 2) e = wide ? launch_range<__bf16, 8, 1024, 2>(p, st) : launch_range<__bf16, 1, 512, 16>(p, st);
-  else e = wide ? launch_range<float, 4, 1024, 2>(p, st) : launch_range<float, 1, 512, 8>(p, st);
-  return e == hipSuccess ? HOOK_OK : HOOK_ERR_LAUNCH;
+  if (esize == 2) return wide ? launch_range<__bf16, 8, 1024, 2>(p, st) : launch_range<__bf16, 1, 512, 16>(p, st);
+  return wide ? launch_range<float, 4, 1024, 2>(p, st) : launch_range<float, 1, 512, 8>(p, st);
 }

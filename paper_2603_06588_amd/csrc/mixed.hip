@@ -58,7 +58,7 @@ hipError_t launch(const AttnParams& p, long long grid, hipStream_t st) {
 hipError_t launch_mixed(const AttnParams& p, int D, hipStream_t st) {
   const long long rows = ((long long)p.dec_ranges * p.Hkv * p.dec_hgroups + 7) & ~7ll;
   const long long grid = rows + (long long)(p.total_q / p.rows_per_wg + p.num_seqs) * p.Hkv * p.hgroups + (p.pf_self ? 1 : 0);
-  if (!grid_fits(grid)) return hipErrorInvalidValue;
+  if (!grid_fits(grid, 256)) return hipErrorInvalidValue;
   if (D == 128) return !p.kv8 ? launch<128, false>(p, grid, st) : launch<128, true>(p, grid, st);
   if (D == 64) return !p.kv8 ? launch<64, false>(p, grid, st) : launch<64, true>(p, grid, st);
   return hipErrorInvalidValue;

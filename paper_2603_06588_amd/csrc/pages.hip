@@ -619,7 +619,9 @@ hook_status hook_pages_fork(const hook_pages_args* a) {
   if (!sizes_ok(a) || a->num_rows < 0) return HOOK_ERR_SHAPE;
   if (!sizes_supported(a)) return HOOK_ERR_UNSUPPORTED;
   const long long chunks = row_chunks_of(a);
-  if (a->num_rows > (1 << 26) || !grid_fits(a->num_rows * chunks + a->max_blocks_per_seq)) return HOOK_ERR_UNSUPPORTED;
+  const int columns = (a->max_blocks_per_seq + kCols - 1) / kCols;
+  const long long workgroups = a->num_rows * chunks + std::min(columns, kCounters);
+  if (a->num_rows > (1 << 26) || !grid_fits(workgroups, kForkThreads)) return HOOK_ERR_UNSUPPORTED;
   const bool no_rows = a->num_rows == 0 && a->num_seqs == 0;
   if (no_rows && a->ref_counts == a->ref_counts_out) return HOOK_OK;
   if (!a->ref_counts || !a->ref_counts_out || !a->status) return HOOK_ERR_NULL;
@@ -638,8 +640,7 @@ hook_status hook_pages_fork(const hook_pages_args* a) {
     if (hipGetLastError() != hipSuccess) return HOOK_ERR_LAUNCH;
   }
   if (no_rows) return HOOK_OK;
-  const int columns = (p.mb + kCols - 1) / kCols;
-  const dim3 grid((unsigned)(p.rows * chunks + std::min(columns, kCounters)));
+  const dim3 grid((unsigned)workgroups);
   if (columns > kCounters) hipLaunchKernelGGL(k_pages_fork<true>, grid, dim3(kForkThreads), 0, st, p, (int)chunks);
   else hipLaunchKernelGGL(k_pages_fork<false>, grid, dim3(kForkThreads), 0, st, p, (int)chunks);
   return hipGetLastError() == hipSuccess ? HOOK_OK : HOOK_ERR_LAUNCH;
@@ -663,7 +664,7 @@ hook_status hook_pages_append(const hook_pages_args* a) {
   int groups = p.ncaches > 0 ? p.ncaches : 1;
   while (groups > 1 && (long long)groups * p.S > 4096) groups = (groups + 1) / 2;
   const int waves = kThreads / 64;
-  if (!grid_fits((long long)p.S * groups)) return HOOK_ERR_UNSUPPORTED;
+  if (!grid_fits((long long)p.S * groups, kThreads)) return HOOK_ERR_UNSUPPORTED;
   if (p.S == 0 && p.refs == p.refs_out) return HOOK_OK;
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   hipLaunchKernelGGL(k_pages_plan, dim3((unsigned)(p.nc + (p.S + waves - 1) / waves)), dim3(kThreads), 0, st, p);
@@ -693,7 +694,7 @@ hook_status hook_pages_compact(const hook_pages_args* a) {
   // Ordinary loads where all caches together fit 256 MB of last-level cache, streaming ones otherwise: 8 caches of 512 pages of 32 KB 16.7 and
   // 18.2 us, of 8192 pages 218 and 205.
   p.keep_lines = (long long)p.ncaches * p.nb * p.heads * kBlock * p.row_chunks * 16 <= (256ll << 20);
-  if (!grid_fits(movers + mappers + p.S * chunks)) return HOOK_ERR_UNSUPPORTED;
+  if (!grid_fits(movers + mappers + p.S * chunks, kThreads)) return HOOK_ERR_UNSUPPORTED;
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   hipLaunchKernelGGL(k_pages_list, dim3((unsigned)p.nc), dim3(kThreads), 0, st, p);
   if (hipGetLastError() != hipSuccess) return HOOK_ERR_LAUNCH;

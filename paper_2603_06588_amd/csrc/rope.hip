@@ -279,13 +279,17 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int p
   }
 }
 
+// Workgroups to a token.  Few tokens: a token's heads are cut over several of them, one round of units each, to be spread over the chip (2000
+// tokens of 32 and 8 heads 14.8 us so, 12.0 with a workgroup each; 1000 tokens 8.5 with either, where the launch counts).
+long long parts_of(const RopeParams& p, int width, bool neighbours) {
+  const long long per_token = (long long)(p.Hq + p.Hk) * units_of(p.d, p.pairs, width, neighbours) + (long long)p.Hv * ((vectors_of(p.d, width) + 1) / 2);
+  return p.T >= 600 ? 1 : (per_token + kRopeThreads - 1) / kRopeThreads;
+}
+
 template <typename E, bool NEIGHBOURS, bool ALIGNED>
 hipError_t launch_rope(const RopeParams& p, hipStream_t st) {
   constexpr int W = 16 / sizeof(E);
-  const long long per_token = (long long)(p.Hq + p.Hk) * units_of(p.d, p.pairs, W, NEIGHBOURS) + (long long)p.Hv * ((vectors_of(p.d, W) + 1) / 2);
-  // Few tokens: a token's heads are cut over several workgroups, one round of units each, to be spread over the chip (2000 tokens of 32 and
-  // 8 heads 14.8 us so, 12.0 with a workgroup each; 1000 tokens 8.5 with either, where the launch counts).
-  const long long parts = p.T >= 600 ? 1 : (per_token + kRopeThreads - 1) / kRopeThreads;
+  const long long parts = parts_of(p, W, NEIGHBOURS);
   hipLaunchKernelGGL((k_rope<E, W, NEIGHBOURS, ALIGNED>), dim3((unsigned)(p.T * parts)), dim3(kRopeThreads), 0, st, p, (int)parts);
   return hipGetLastError();
 }
@@ -394,12 +398,11 @@ extern "C" hook_status hook_rope(const hook_rope_args* a) {
     divides((uintptr_t)a->v_cache * (kv8 ? 2 : 1));
   }
   if (grain % esize != 0) return HOOK_ERR_UNSUPPORTED;
+  const bool neighbours = a->layout == HOOK_ROPE_NEIGHBOURS, aligned = grain % 16 == 0;
   // (an upper bound of the units of a token: one to a vector)
-  if (!grid_fits(((long long)(p.Hq + p.Hk + p.Hv) * (a->head_dim * esize / 16 + 3) / kRopeThreads + 1) * (p.T < 600 ? p.T : 1)) ||
-      (long long)(p.Hq + p.Hk + p.Hv) * (a->head_dim * esize / 16 + 3) > (1 << 27))
+  if ((long long)(p.Hq + p.Hk + p.Hv) * (a->head_dim * esize / 16 + 3) > (1 << 27) || !grid_fits(p.T * parts_of(p, 16 / esize, neighbours), kRopeThreads))
     return HOOK_ERR_UNSUPPORTED;
   hipStream_t st = static_cast<hipStream_t>(a->stream);
-  const bool neighbours = a->layout == HOOK_ROPE_NEIGHBOURS, aligned = grain % 16 == 0;
   const hipError_t e = a->dtype == HOOK_BF16 ? launch_rope<__bf16>(p, neighbours, aligned, st) : launch_rope<float>(p, neighbours, aligned, st);
   return e == hipSuccess ? HOOK_OK : HOOK_ERR_LAUNCH;
 }

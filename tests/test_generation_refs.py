@@ -274,3 +274,24 @@ def test_fork_of_no_rows_still_needs_both_counts(binding):
     none = dict(num_seqs=0, num_rows=0)
     assert fork(_pages(binding, **none, ref_counts_out=0)) == 1 and fork(_pages(binding, **none, ref_counts=0)) == 1
     assert fork(_pages(binding, **none, ref_counts=0, ref_counts_out=0)) == 0     # no counts that could change
+
+
+def test_sizes_beyond_a_launch_are_refused(binding):
+    """2^32 threads or more, in workgroups of 256 (rotation, append, compact, capture), 512 and 1024 (logits) and 1024 (fork); nothing is launched."""
+    lib = binding.load_library()
+    assert _rope(binding, num_tokens=1 << 24, q_out=2 * P, k_out=2 * P) == 3
+    assert _rope(binding, num_tokens=599, num_q_heads=65536, num_kv_heads=65536, head_dim=512, rotary_dim=0, axis_pairs=(0,), dtype=1, q_out=2 * P,
+                 k_out=2 * P) == 3                                                # 32768 workgroups to a token
+    assert lib.hook_pages_fork(_pages(binding, num_rows=1 << 22)) == 3
+    assert lib.hook_pages_fork(_pages(binding, num_rows=1 << 19, max_blocks_per_seq=8192)) == 3
+    in_place = dict(num_seqs=1 << 24, block_table_out=P, seq_lens_out=2 * P, workspace_bytes=1 << 40)
+    for call in (lib.hook_pages_append, lib.hook_pages_compact):
+        assert call(_pages(binding, **in_place)) == 3
+    assert _logits(binding, num_rows=1 << 22, vocab=8) == 3
+    assert _logits(binding, num_rows=1 << 23, vocab=8, out=P + 2) == 3            # rows off the borders: single elements
+    assert _logits(binding, num_rows=1 << 20, vocab=32769, dtype=1, out=P + 4) == 3
+    a = binding.HookCaptureQkArgs()
+    for key, v in dict(num_seqs=1 << 20, total_q=1 << 20, num_q_heads=64, num_kv_heads=8, head_dim=128, block_size=16, max_blocks_per_seq=4, num_blocks=4,
+                       num_probe_heads=64, max_sel_q=64, q=P, cu_q_lens=P, probe_heads=P, query_sel=P, q_out=P).items():
+        setattr(a, key, v)
+    assert lib.hook_capture_qk(a) == 3
