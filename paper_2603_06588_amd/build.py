@@ -52,10 +52,10 @@ def build_lib(verbose: bool = False, jobs: int = 8) -> str:
     with ThreadPoolExecutor(max_workers=jobs) as pool:
         tensors = pool.submit(_build_tensors)
         objs = list(pool.map(_compile, SOURCES + BENCH_SOURCES))
-        tensors.result()
     product, bench = objs[:len(SOURCES)], objs[len(SOURCES):]
     _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *product, "-o", LIB])
     _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *product, *bench, "-o", BENCH_LIB])
+    tensors.result()      # (the libraries are there by then, whatever became of the front end's part)
     if verbose:
         print("hipcc", " ".join(FLAGS), "-c csrc/*.hip ->", LIB, "and", BENCH_LIB)
     return LIB
