@@ -557,6 +557,7 @@ def hook_steer(hidden: torch.Tensor, vec: torch.Tensor, alpha: float, token_mask
 # (csrc/tensors.cpp: same GPU, types, layouts; an address and sizes for each), and the struct is filled in another.
 
 _look_fn = None
+_INT32_MAX = 0x7FFFFFFF      # sizes are 32 bits in the structs, which would take a larger one modulo 2^32
 
 
 def _look(where: str, like, spec, *tensors):
@@ -642,7 +643,10 @@ def hook_rope(q, k, positions, inv_freq, axis_pairs=None, layout: int = ROPE_HAL
         num_seqs, max_blocks, num_blocks, block_size = nlens, tn[1], kcn[0], kcn[2]
     else:
         vp = table = lens = cu = 0
-    a = HookRopeArgs(T, qn[1] if qn else 0, kn[1] if kn else 0, d, 2 * pairs, axes, _FourInts(*axis_pairs), layout, axis_order, 1 if inverse else 0,
+    hq, hkv = qn[1] if qn else 0, kn[1] if kn else 0
+    if (T | hq | hkv | d | 2 * pairs | num_seqs | max_blocks | num_blocks | block_size) > _INT32_MAX:
+        raise HookError(3, "hook_rope (sizes)")
+    a = HookRopeArgs(T, hq, hkv, d, 2 * pairs, axes, _FourInts(*axis_pairs), layout, axis_order, 1 if inverse else 0,
                      _DT[dt], magnitude, pos, freq, qp, kp, qop, kop, qs, ks, qos, kos, num_seqs, block_size, max_blocks, num_blocks, vp, vs, table,
                      lens, cu, kc, vc, kv_dtype, ksc, vsc)
     _launch((_lib or load_library()).hook_rope, a, index, stream, where)
@@ -670,6 +674,8 @@ def _pages_args(where: str, block_table, seq_lens, ref_counts, table_out, lens_o
             (src_lens is not None and ncut != rows) or (cu_q_lens is not None and ncu != num_seqs + 1) or
             (page_map is not None and (npm != num_blocks or nlive != 1))):
         raise HookError(2, f"{where} (shape)")
+    if (num_seqs | max_blocks | num_blocks | rows) > _INT32_MAX:
+        raise HookError(3, f"{where} (sizes)")
     return HookPagesArgs(num_seqs, max_blocks, num_blocks, 16, table, lens, refs, to, lens_to, refs_to, st, rows, src, cut, cu, pm, live), index
 
 
@@ -697,6 +703,8 @@ def _pages_data(where: str, a, caches, like, workspace, index: int, stream):
             raise HookError(2, f"{where} (caches: shape)")
         if n > 1 and any(s != shape for s in seen[4:-2:2]) or any(c.dtype is not dtype for c in each):
             raise HookError(2, f"{where} (caches: shape, dtype)")
+        if shape[-3] > _INT32_MAX:
+            raise HookError(3, f"{where} (caches: sizes)")
         a.num_kv_heads, a.row_bytes = shape[-3], shape[-1] * each[0].element_size()
         if stacked:
             n, step = shape[0], shape[1] * shape[2] * 16 * a.row_bytes
@@ -771,6 +779,9 @@ def hook_steer_logits(logits, out=None, history=None, cu_history=None, prompt_le
             (frequency is not None and nfr != rows) or (presence is not None and npr != rows) or (cu_bias is not None and ncub != rows + 1) or nbi != nbv or
             (mask_rows is not None and nmr != rows) or (mask is not None and (mask.dim() != 2 or mask.shape[1] != words))):
         raise HookError(2, "hook_steer_logits (shape)")
-    a = HookSteerLogitsArgs(rows, vocab, _DT[dt], x, y, xs, ys, nh, h, cuh, pl, rep, fr, pr, nbi, cub, bi, bv, nm // words if words else 0, m, mr)
+    masks = nm // words if words else 0
+    if (rows | vocab | nh | nbi | masks) > _INT32_MAX:
+        raise HookError(3, "hook_steer_logits (sizes)")
+    a = HookSteerLogitsArgs(rows, vocab, _DT[dt], x, y, xs, ys, nh, h, cuh, pl, rep, fr, pr, nbi, cub, bi, bv, masks, m, mr)
     _launch((_lib or load_library()).hook_steer_logits, a, index, stream, where)
     return out
