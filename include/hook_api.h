@@ -484,8 +484,8 @@ hook_status hook_reduce_mass(const hook_reduce_args* args);
  * angle
  *   a(t, c) = positions[axis(c), t] * inv_freq[c]          c in [0, rotary_dim / 2)
  *   (x1, x2) -> m * (x1 cos a - x2 sin a, x2 cos a + x1 sin a)       m = magnitude, or 1 where that is 0
- * and with `inverse` by -a (captured queries and keys turned back; also the gradient of the rotation with respect to its
- * input, for m = 1).  Elements rotary_dim .. head_dim - 1 of a head pass unchanged.  The angle is reduced in fp64, so far positions lose
+ * and with `inverse` by -a.  That is the gradient of the call with respect to its input, with the same magnitude; captured queries and
+ * keys are turned back by it with magnitude 1 / m.  Elements rotary_dim .. head_dim - 1 of a head pass unchanged.  The angle is reduced in fp64, so far positions lose
  * nothing; the rotation is computed in fp32 and rounded once, to nearest even.
  *   layout      HOOK_ROPE_HALVES: pair c is elements c and c + rotary_dim / 2; HOOK_ROPE_NEIGHBOURS: 2c and 2c + 1
  *   axis_order  HOOK_ROPE_BLOCKED: the first axis_pairs[0] pairs belong to axis 0, the next axis_pairs[1] to axis 1, ...;

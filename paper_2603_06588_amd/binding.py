@@ -592,7 +592,8 @@ def hook_rope(q, k, positions, inv_freq, axis_pairs=None, layout: int = ROPE_HAL
               inverse: bool = False, magnitude: float = 0.0, q_out=None, k_out=None, v=None, block_table=None, seq_lens=None,
               cu_q_lens=None, k_cache=None, v_cache=None, k_scale=None, v_scale=None, stream=None):
     """Turns q [T, Hq, d] and k [T, Hkv, d] by positions ([T] or [axes, T], int32) times inv_freq (fp32; twice as many elements of a
-    head turn); either may be None.  In place where no output is given.  With k_cache and v_cache the turned keys and v also
+    head turn); either may be None.  In place where no output is given.  ``inverse`` with the same magnitude is the call's gradient, with
+    one over it the way back.  With k_cache and v_cache the turned keys and v also
     go to the cache, as by ``hook_kv_write``; k itself is then left alone unless it is k_out.  Rows may be views into a wider
     buffer.  Returns (q_out, k_out)."""
     where = "hook_rope"

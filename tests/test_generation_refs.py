@@ -295,3 +295,18 @@ def test_sizes_beyond_a_launch_are_refused(binding):
                        num_probe_heads=64, max_sel_q=64, q=P, cu_q_lens=P, probe_heads=P, query_sel=P, q_out=P).items():
         setattr(a, key, v)
     assert lib.hook_capture_qk(a) == 3
+
+
+@pytest.mark.parametrize("m", [1.0, 1.25])
+def test_inverse_with_a_magnitude(m):
+    """By the same magnitude the gradient, by one over it the way back."""
+    g = torch.Generator().manual_seed(5)
+    x, w = torch.randn((2, 1, 6), generator=g).double(), torch.randn((2, 1, 6), generator=g).double()
+    f, pos = torch.tensor([1.0, 0.3], dtype=torch.float64), torch.tensor([3, -4])
+    assert torch.allclose(G.rope(G.rope(x, pos, f, magnitude=m), pos, f, inverse=True, magnitude=1 / m), x, atol=1e-12)
+    want = G.rope(w, pos, f, inverse=True, magnitude=m)
+    for i in range(x.numel()):
+        h = torch.zeros_like(x)
+        h.view(-1)[i] = 1e-5
+        slope = ((G.rope(x + h, pos, f, magnitude=m) - G.rope(x - h, pos, f, magnitude=m)) * w).sum() / 2e-5
+        assert abs(float(slope) - float(want.reshape(-1)[i])) < 1e-9
