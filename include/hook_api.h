@@ -569,8 +569,9 @@ typedef enum hook_pages_status {
   HOOK_PAGES_FULL = 1,       /* append: too few free pages, or a row longer than the table; nothing was done */
   HOOK_PAGES_BAD_ROW = 2,    /* fork: src_rows[j] outside [-1, num_seqs); the new row is empty */
   HOOK_PAGES_BAD_LENGTH = 4, /* a length outside [0, max_blocks_per_seq * 16], taken as the nearest of these, or a negative n_i, taken as 0 */
-  HOOK_PAGES_BAD_PAGE = 8    /* a page that a row holds is outside [0, num_blocks) (its number is carried along), or, in
-                                hook_pages_compact, free (the entry is carried along) */
+  HOOK_PAGES_BAD_PAGE = 8    /* a page outside [0, num_blocks), or in compact a free one; its entry is carried along.  fork looks at all pages
+                                that the old rows hold and the new ones take, compact at all that the rows hold, append at the last
+                                page of a row that is to take new tokens into it and at no other */
 } hook_pages_status;
 
 #define HOOK_PAGES_MAX_CACHES 256

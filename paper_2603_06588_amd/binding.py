@@ -680,7 +680,7 @@ def _pages_args(where: str, block_table, seq_lens, ref_counts, table_out, lens_o
     return HookPagesArgs(num_seqs, max_blocks, num_blocks, 16, table, lens, refs, to, lens_to, refs_to, st, rows, src, cut, cu, pm, live), index
 
 
-_CACHES: dict = {}      # "caches[0]", "caches[1]", ... as often as the longest list so far
+_CACHES: dict = {}      # by the length of a list of caches: what _look is to look for in them and in the scratch
 
 
 def _pages_data(where: str, a, caches, like, workspace, index: int, stream):

@@ -18,7 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kChunk = 2048;          // pages of a workgroup, eight to a thread
 constexpr int kPer = kChunk / kThreads;
-constexpr int kRowChunk = 1024;       // table entries of a workgroup, four to a thread
+constexpr int kRowChunk = 1024;       // table entries of a workgroup, one to a thread in fork and four in compact
 constexpr int kTooMany = 0x3fffffff;  // "needs" of a row that the table cannot hold: more than any cache has
 
 struct RowPlan {

@@ -310,3 +310,10 @@ def test_inverse_with_a_magnitude(m):
         h.view(-1)[i] = 1e-5
         slope = ((G.rope(x + h, pos, f, magnitude=m) - G.rope(x - h, pos, f, magnitude=m)) * w).sum() / 2e-5
         assert abs(float(slope) - float(want.reshape(-1)[i])) < 1e-9
+
+
+def test_append_looks_at_the_last_page_alone():
+    # page 99 lies outside: full in row 0, the last one of rows that take nothing and that begin a new page, and one that takes a token
+    rows, lens, refs, copies, status = G.append([0, 1, 1, 2], [[99, 0, 7], [99, 7, 7], [99, 7, 7]], [20, 9, 16], [1, 0, 0])
+    assert rows == [[99, 0], [99], [99, 1]] and lens == [21, 9, 17] and refs == [1, 1, 0] and status == 0 and copies == []
+    assert G.append([0, 1], [[99, 7]], [9], [1, 0, 0])[4] == G.BAD_PAGE

@@ -475,3 +475,12 @@ def test_fork_of_no_rows_into_no_rows_hands_the_counts_on(mb):
     assert counts.tolist() == refs.tolist() == [3, 0, 1] * 100 and int(status) == 0
     binding.hook_pages_fork(empty, none, empty, refs, none.clone(), empty.clone(), status)
     assert refs.tolist() == [3, 0, 1] * 100 and int(status) == 0
+
+
+def test_append_looks_at_the_last_page_alone():
+    table, lens, refs, cu = [[99, 0, 7], [99, 7, 7], [99, 7, 7]], [20, 9, 16], [1, 0, 0], [0, 1, 1, 2]
+    t, L, c, status = ints(table), ints(lens), ints(refs), ints([0])
+    binding.hook_pages_append(ints(cu), t, L, c, [], status)
+    rows, want_l, want, _, bits = G.append(cu, table, lens, refs)
+    check_table(t, rows, table)
+    assert L.tolist() == want_l and c.tolist() == want and int(status) == bits == 0
