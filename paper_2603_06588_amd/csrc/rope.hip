@@ -7,7 +7,7 @@
 // by units of two vectors of what one load carries: the two halves of as many pairs, or neighbouring pairs in each.  The
 // first units are requested before the angles are computed.
 // 16384 tokens of 64 query and 8 key and value heads of 128 into the cache: 120 us, 5.9 TB/s (two tokens to a workgroup 123, four 137;
-// threads 128 / 512: 127 / 139); 8000 tokens of 32 and 8: 40 us, neighbouring pairs 39, 8-bit cache 43.
+// threads 128 / 512: 127 / 139); 8000 tokens of 32 and 8: 40 us, neighbouring pairs 39, 8-bit cache 45.
 #include "../../include/hook_api.h"
 #include "kv_write_device.h"
 
@@ -116,8 +116,8 @@ __device__ __forceinline__ int find_sequence(const int* cu, int n, int row, int 
 // ALIGNED: pairs and heads are whole vectors, and every vector lies at a multiple of 16 bytes.  Otherwise vectors lie anywhere (the
 // memory takes them at any address) and the last one of the pairs, of what is behind them and of a head may be a part of one.  Such a
 // part is moved back to be a whole one, whose first elements another thread computes alike, unless those are turned in place or
-// there are not as many (8000 tokens of 32 + 8 heads with 25 pairs, halves: 63 us, 87 with parts by elements;
-// neighbours 51).
+// there are not as many (8000 tokens of 32 + 8 heads with 25 pairs into the cache, halves: 62 us, 88 with parts by elements;
+// neighbours 51).  What goes to and from memory is the same as with whole vectors (83 + 82 MB without the cache).
 template <typename E, int W, bool NEIGHBOURS, bool ALIGNED>
 __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int parts) {
   __shared__ float sh_cos[HOOK_ROPE_MAX_DIM / 2], sh_sin[HOOK_ROPE_MAX_DIM / 2];
@@ -279,8 +279,12 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeParams p, int p
   }
 }
 
-// Workgroups to a token.  Few tokens: a token's heads are cut over several of them, one round of units each, to be spread over the chip (2000
-// tokens of 32 and 8 heads 14.8 us so, 12.0 with a workgroup each; 1000 tokens 8.5 with either, where the launch counts).
+// Workgroups to a token.  Few tokens: a token's heads are cut over several of them, one round of units each, to be spread over the chip; many fill it
+// with one each, whose angles and slot are then found once.  Cut / whole, launches of a graph on the same tensors, 128 elements into the cache:
+//   tokens         64         256        500        600        700        1000         2000
+//   32 + 8 heads   3.2 / 3.9  3.8 / 4.2  4.9 / 4.9  5.2 / 5.1  6.1 / 5.1   8.1 / 5.4   13.1 / 9.9  us
+//   64 + 8 heads   3.2 / 4.7  4.3 / 5.5  5.9 / 6.0  7.0 / 7.5  8.5 / 7.9  10.5 / 9.3   17.7 / 15.9
+// A token of no more units than a workgroup has threads (8 + 1 heads) is not cut on either side.
 long long parts_of(const RopeParams& p, int width, bool neighbours) {
   const long long per_token = (long long)(p.Hq + p.Hk) * units_of(p.d, p.pairs, width, neighbours) + (long long)p.Hv * ((vectors_of(p.d, width) + 1) / 2);
   return p.T >= 600 ? 1 : (per_token + kRopeThreads - 1) / kRopeThreads;
