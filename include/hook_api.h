@@ -34,8 +34,8 @@
  *     bad table cannot fault, lengths beyond the table are clamped, and the
  *     condition is recorded in the workspace (see hook_attn_probe_device_status;
  *     hook_attn_probe_validate checks the contents on request).
- *   - A launch takes fewer than 2^32 threads.  Sizes that need more (hook_rope: more than 2^24 - 1 tokens) are refused with
- *     HOOK_ERR_UNSUPPORTED.
+ *   - A launch takes fewer than 2^32 threads.  hook_rope (2^24 - 1 tokens at most), hook_pages_fork, hook_pages_append, hook_pages_compact,
+ *     hook_steer_logits and hook_capture_qk refuse sizes that need more with HOOK_ERR_UNSUPPORTED, the others end with HOOK_ERR_LAUNCH.
  *   - One call covers one layer; [layer, head] lists (Section 2, config example)
  *     are split per layer by the caller.
  */

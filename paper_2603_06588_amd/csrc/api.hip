@@ -250,10 +250,11 @@ __attribute__((visibility("hidden"))) hook_status run_attn_probe(const hook_attn
   const int P = a->num_probe_heads;
   const bool kv8 = a->kv_dtype == HOOK_KV_FP8_E4M3;
   const Layout l = make_layout(a, workspace_bytes);
-  // one-dimensional launch grids over the item capacities
+  // one-dimensional launch grids over the item capacities (of which a batch of one kind launches one, and a streaming one less:
+  // the launches look at their own threads)
   if (a->dtype == HOOK_BF16 &&
-      (!grid_fits((long long)l.pf_cap * a->num_kv_heads * l.hgroups, 64 * l.pf_waves) ||
-       !grid_fits((long long)l.dec_cap * a->num_kv_heads * l.dec_hgroups, 256)))
+      (!grid_fits((long long)l.pf_cap * a->num_kv_heads * l.hgroups, 1) ||
+       !grid_fits((long long)l.dec_cap * a->num_kv_heads * l.dec_hgroups, 1)))
     return HOOK_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < l.needed || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0)
     return HOOK_ERR_WORKSPACE;

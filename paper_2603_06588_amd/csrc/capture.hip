@@ -147,7 +147,7 @@ extern "C" hook_status hook_capture_qk(const hook_capture_qk_args* a) {
   if (do_k) {
     if (!a->k_cache || !a->block_table || !a->seq_lens || !a->capture_kv_heads || !a->cu_k_lens || !a->k_out)
       return HOOK_ERR_NULL;
-    if ((long long)kTokTile * p.KH * p.row_chunks > 0x7FFFFFFFll) return HOOK_ERR_UNSUPPORTED;
+    if ((long long)kTokTile * p.KH * p.row_chunks > 0x7FFFFFFFll || !grid_fits(((long long)p.total_k + kTokTile - 1) / kTokTile, 256)) return HOOK_ERR_UNSUPPORTED;
   }
   if (do_q) {
     hipLaunchKernelGGL(k_capture_q, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, p);

@@ -295,6 +295,15 @@ def test_sizes_beyond_a_launch_are_refused(binding):
                        num_probe_heads=64, max_sel_q=64, q=P, cu_q_lens=P, probe_heads=P, query_sel=P, q_out=P).items():
         setattr(a, key, v)
     assert lib.hook_capture_qk(a) == 3
+    a.max_sel_q, a.num_capture_kv_heads, a.total_k = 1, 1, (1 << 28) + 16
+    a.k_cache = a.block_table = a.seq_lens = a.capture_kv_heads = a.cu_k_lens = a.k_out = P
+    assert lib.hook_capture_qk(a) == 3                                            # (2^30 threads for the queries: those alone would run)
+    # an attention call of one kind is not held to the threads of the other (no workspace: nothing is launched)
+    attn = binding.HookAttnProbeArgs()
+    for key, v in dict(num_seqs=300000, total_q=300000, num_q_heads=256, num_kv_heads=32, head_dim=64, block_size=16, max_blocks_per_seq=4, num_blocks=4,
+                       batch_kind=binding.BATCH_DECODE_ONLY, q=P, k_cache=P, v_cache=P, block_table=P, seq_lens=P, cu_q_lens=P, out=P).items():
+        setattr(attn, key, v)
+    assert lib.hook_attn_probe(attn) == 4
 
 
 @pytest.mark.parametrize("m", [1.0, 1.25])
