@@ -235,7 +235,10 @@ _SAME = contextlib.nullcontext()
 def _taken_on(stream):
     """Where a call on `stream` takes new memory from: that stream's own pool.  A block of another stream's may be one that has just been given
     back there while work queued on it still uses the block, and nothing orders the call behind that work."""
-    return _SAME if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return _SAME
+    # (another program's stream, known by its handle alone, will do)
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream.cuda_stream)))
 
 
 def _handed_over(stream, *results):
@@ -243,7 +246,7 @@ def _handed_over(stream, *results):
     memory is not given to anybody else before that is done."""
     if stream is not None and results:
         current = torch.cuda.current_stream(results[0].device)
-        if current != stream:
+        if current.cuda_stream != int(stream.cuda_stream):
             for t in results:
                 t.record_stream(current)
 

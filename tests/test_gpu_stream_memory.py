@@ -47,3 +47,7 @@ def test_a_call_on_another_stream(name, taken):
     assert taken and all(s == side for s in taken) and torch.cuda.current_stream() != side
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(bits(x), bits(y)) for x, y in zip(got, want))
+    got = call(type("Handle", (), {"cuda_stream": side.cuda_stream}))      # a stream known by its handle alone
+    assert all(s.cuda_stream == side.cuda_stream for s in taken)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(bits(x), bits(y)) for x, y in zip(got, want))

@@ -1,18 +1,24 @@
 """Where the Python calls take memory from when they are given a stream: from that stream's pool, so that a block is never one that another
 stream has given back with work still queued on it.  The library and the streams are stand-ins here (no GPU)."""
-import types
-
 import pytest
 import torch
 
 from paper_2603_06588_amd import binding
 
 
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+CURRENT = Stream(5)
+
+
 class Streams:
     """The current stream's name, as torch.cuda.stream() switches it."""
 
     def __init__(self):
-        self.current, self.taken, self.recorded = "current", [], []
+        self.current, self.taken, self.recorded = CURRENT, [], []
 
     def switch(self, stream):
         outer = self
@@ -47,6 +53,8 @@ def streams(monkeypatch):
     monkeypatch.setattr(binding.torch, "empty", on_host(torch.empty))
     monkeypatch.setattr(binding.torch, "empty_like", on_host(torch.empty_like))
     monkeypatch.setattr(torch.cuda, "stream", s.switch)
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: s.current)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: s.recorded.append((stream, t)))
     monkeypatch.setattr(binding, "load_library", Library)
@@ -68,23 +76,27 @@ def calls():
     }
 
 
+class Handle:
+    cuda_stream = 77
+
+
 @pytest.mark.parametrize("name", list(calls()))
-def test_memory_comes_from_the_stream_of_the_call(name, streams, monkeypatch):
+@pytest.mark.parametrize("known", [True, False])      # a torch stream, and an object that has its handle alone
+def test_memory_comes_from_the_stream_of_the_call(name, known, streams, monkeypatch):
     call, results, allocations = calls()[name]
-    stream = types.SimpleNamespace(cuda_stream=77)
+    stream = Stream(77) if known else Handle()
     monkeypatch.setattr(binding, "_stream_handle", lambda s: 77)
     out = call(stream)
-    assert len(streams.taken) == allocations and all(on is stream for on, _ in streams.taken)
+    assert len(streams.taken) == allocations and all(on.cuda_stream == 77 for on, _ in streams.taken)
     # results outlive the call and are read on the current stream, scratch is not
     assert len(out) == results and {id(t) for t in out} == {id(t) for _, t in streams.recorded}
-    assert all(on == "current" for on, _ in streams.recorded)
+    assert all(on is CURRENT for on, _ in streams.recorded)
 
 
 @pytest.mark.parametrize("name", list(calls()))
 @pytest.mark.parametrize("given", [False, True])
 def test_calls_on_the_current_stream_record_nothing(name, given, streams, monkeypatch):
     call, _, allocations = calls()[name]
-    streams.current = types.SimpleNamespace(cuda_stream=5) if given else "current"
     monkeypatch.setattr(binding, "_stream_handle", lambda s: 5)
-    call(streams.current if given else None)
-    assert len(streams.taken) == allocations and all(on is streams.current for on, _ in streams.taken) and not streams.recorded
+    call(CURRENT if given else None)
+    assert len(streams.taken) == allocations and all(on is CURRENT for on, _ in streams.taken) and not streams.recorded
