@@ -232,13 +232,13 @@ def _stream_handle(stream) -> int:
 _SAME = contextlib.nullcontext()
 
 
-def _taken_on(stream):
-    """Where a call on `stream` takes new memory from: that stream's own pool.  A block of another stream's may be one that has just been given
+def _taken_on(stream, device):
+    """Where a call on `stream` takes new memory of `device` from: that stream's own pool.  A block of another stream's may be one that has just been given
     back there while work queued on it still uses the block, and nothing orders the call behind that work."""
     if stream is None:
         return _SAME
     # (another program's stream, known by its handle alone, will do)
-    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream.cuda_stream)))
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream.cuda_stream), device=device))
 
 
 def _handed_over(stream, *results):
@@ -336,7 +336,7 @@ def hook_attn_probe(q, k_cache, v_cache, block_table, seq_lens, cu_q_lens, probe
                     query_sel=None, max_spans=1, key_spans=None, scale: float = 0.0,
                     stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(out, mass) of one layer's hooked attention; asynchronous on the current stream."""
-    with _taken_on(stream):
+    with _taken_on(stream, q.device):
         call = AttnProbeCall(q, k_cache, v_cache, block_table, seq_lens, cu_q_lens, probe_heads, max_sel_q,
                              query_sel, max_spans, key_spans, scale)
     call.launch(stream)
@@ -359,7 +359,7 @@ def hook_span_mass(q, k_cache, block_table, seq_lens, cu_q_lens, probe_heads, ma
         raise HookError(3, "hook_span_mass (dtype)")
     results = ()
     if mass is None:
-        with _taken_on(stream):
+        with _taken_on(stream, q.device):
             mass = torch.empty((num_seqs, P, int(max_sel_q), int(max_spans)), dtype=torch.float32, device=q.device)
         results = (mass,)
     a = HookAttnProbeArgs()
@@ -376,7 +376,7 @@ def hook_span_mass(q, k_cache, block_table, seq_lens, cu_q_lens, probe_heads, ma
         a.kv_dtype, a.k_scale = KV_FP8_E4M3, _p(k_scale)
     if workspace is None and use_workspace:
         need = int(lib.hook_span_mass_workspace_bytes(ctypes.byref(a)))
-        with _taken_on(stream):
+        with _taken_on(stream, q.device):
             workspace = torch.empty(max(need, 8), dtype=torch.uint8, device=q.device) if need else None
     if workspace is not None:
         a.workspace, a.workspace_bytes = _p(workspace), workspace.numel()
@@ -451,7 +451,7 @@ def hook_capture_qk(q, k_cache, block_table, seq_lens, cu_q_lens, probe_heads, m
     P = int(probe_heads.numel()) if probe_heads is not None else 0
     KH = int(capture_kv_heads.numel()) if capture_kv_heads is not None else 0
     results = []
-    with _taken_on(stream):
+    with _taken_on(stream, q.device):
         if q_out is None:
             q_out = torch.empty((num_seqs, P, int(max_sel_q), d), dtype=q.dtype, device=q.device)
             results.append(q_out)
@@ -486,7 +486,7 @@ def hook_reduce_mass(mass, mode: int, span_a: int = 0, span_b: int = 1, query_se
         if accumulate:
             raise ValueError("accumulate needs an existing scores tensor")
         shape = (num_seqs, S) if mode == REDUCE_SPAN_MEAN else (num_seqs,)
-        with _taken_on(stream):
+        with _taken_on(stream, mass.device):
             scores = torch.empty(shape, dtype=torch.float32, device=mass.device)
         results = (scores,)
     a = HookReduceArgs()
@@ -696,7 +696,7 @@ def _pages_data(where: str, a, caches, like, workspace, index: int, stream):
     if spec is None:
         spec = _CACHES[n] = tuple(f"ccaches[{i}]" for i in range(n)) + ("cworkspace",)
     if workspace is None:
-        with _taken_on(stream):
+        with _taken_on(stream, index):
             workspace = torch.empty(pages_workspace_bytes(a.num_seqs, a.num_blocks), dtype=torch.uint8, device=index)
     seen = _look(where, like, spec, *each, workspace)
     a.workspace, a.workspace_bytes = seen[-2], workspace.numel() * workspace.element_size()

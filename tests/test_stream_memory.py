@@ -7,8 +7,8 @@ from paper_2603_06588_amd import binding
 
 
 class Stream:
-    def __init__(self, handle):
-        self.cuda_stream = handle
+    def __init__(self, handle, device=None):
+        self.cuda_stream, self.device = handle, device
 
 
 CURRENT = Stream(5)
@@ -88,6 +88,8 @@ def test_memory_comes_from_the_stream_of_the_call(name, known, streams, monkeypa
     monkeypatch.setattr(binding, "_stream_handle", lambda s: 77)
     out = call(stream)
     assert len(streams.taken) == allocations and all(on.cuda_stream == 77 for on, _ in streams.taken)
+    # a stream known by its handle alone belongs to the GPU of the call's tensors
+    assert known or all(on.device in (0, torch.device("cpu")) for on, _ in streams.taken)
     # results outlive the call and are read on the current stream, scratch is not
     assert len(out) == results and {id(t) for t in out} == {id(t) for _, t in streams.recorded}
     assert all(on is CURRENT for on, _ in streams.recorded)
